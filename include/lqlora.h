@@ -87,7 +87,7 @@ enum { LQ_VARIANT_SPLIT = 0, LQ_VARIANT_FUSED = 1, LQ_VARIANT_SHRINK_ONLY = 2, L
 
 const char* lora_status_string(lq_status status);
 
-/* One size that serves every call of this header on a batch of these dimensions (the largest of
+/* One size that serves every call of this header (but the cache's, which have sizers of their own) on a batch of these dimensions (the largest of
  * lora_build_workspace_bytes, lora_forward_workspace_bytes for every variant, and
  * lora_backward_workspace_bytes): a caller that keeps one workspace per stream needs nothing else.
  * The per-call sizers below give the exact requirement of each call. */
@@ -326,6 +326,112 @@ lq_status lora_split_rows(const void* src, int64_t ld, int32_t d, const int32_t*
 lq_status lora_concat_rows(const void* parts, int32_t d, const int32_t* perm, int32_t n_tokens,
                            const int32_t* seg_starts, const int32_t* n_segments, int32_t max_segments,
                            void* dst, int64_t ld, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Paged key/value cache in 8 bits, and attention over it: what Algorithm 1's flow has between the q,k,v
+ * projections and the output projection for the prefill (and evaluation) and decode rows.
+ *
+ * A page holds page_tokens positions of all key/value heads of ONE layer; a layer's pages lie in one
+ * device buffer of n_pages * lora_cache_page_bytes() bytes (its pool).  The page table, the lengths and
+ * the reference counts are common to the layers:
+ *   table  int32[n_slots, max_pages]  page of positions j * page_tokens .. of a slot's sequence
+ *   lens   int32[n_slots]             positions that the slot's sequence has (0: the slot is empty)
+ *   refs   int32[n_pages]             slots that hold the page; 0 = free.  All zero, with all lengths zero,
+ *                                     is an empty cache.
+ * Page, with d = head_dim, T = page_tokens, blocks of LQ_CACHE_BLOCK positions:
+ *   [head]{ K codes: byte (t, c) at t * d + c;  V codes: byte (t, c) at (t / 4) * 4 d + 4 c + t % 4 }  2 T d bytes each,
+ *   then [head][block]{ K exponent, V exponent } bytes, padded to a multiple of 128 bytes.
+ * An element's value is e4m3(code) * 2^(exponent - 127) (e4m3: 4 exponent bits with bias 7, 3 mantissa bits, no
+ * infinities, 0x7f and 0xff NaN).  The scale is a power of two, so that a block's scale can grow under the codes that it
+ * holds already at the cost of an exponent, and a value is exact in bf16.
+ *
+ * head_dim 64 or 128, page_tokens 16, 32, 64, 128 or 256, n_kv_heads up to LQ_CACHE_MAX_HEADS, up to 2^22
+ * pages, max_pages * page_tokens up to 2^30 (else LQ_ERR_UNSUPPORTED).
+ * host_cache is read during the call and not kept.  Every call takes a workspace of at least LQ_CACHE_MIN_WORKSPACE bytes,
+ * of which the first 4096 must be ZERO before the first call that uses it (as for the forward, whose workspace may
+ * serve here and the other way round); word 0 is the error word.  Bit 0: a table entry, slot, page or range that cannot be
+ * used (skipped, nothing out of range is touched); bit 2: the free pages ran out.  The calls may be captured into
+ * a graph.  Calls that change the tables or the same pages are ordered by the caller (one stream).
+ *
+ * Rows of a step: span s covers rows row_starts[s] .. row_starts[s + 1] - 1 of the row matrices (int32[n_seqs + 1], not
+ * decreasing, at most n_rows) and the positions first[s], first[s] + 1, ... of slot slots[s]'s sequence (slots NULL: slot s).
+ * Positions have to lie below the slot's length (lora_cache_reserve raises it before the rows are stored); a span
+ * that does not fit is skipped and reported.  Rows of no span are neither read nor written.
+ * ------------------------------------------------------------------------------------------- */
+#define LQ_CACHE_BLOCK 16
+#define LQ_CACHE_MAX_HEADS 256
+#define LQ_CACHE_MIN_WORKSPACE 4096
+
+typedef struct {
+    int32_t n_kv_heads, head_dim, page_tokens;
+    int32_t n_pages, n_slots, max_pages;
+    int32_t* table; /* device */
+    int32_t* lens;  /* device */
+    int32_t* refs;  /* device */
+} lq_cache;
+
+/* bytes of a page of one layer; 0 where the sizes are not supported */
+size_t lora_cache_page_bytes(int32_t n_kv_heads, int32_t head_dim, int32_t page_tokens);
+
+/* workspace of the calls below but the attention, for up to n_seqs slots or spans in a call */
+size_t lora_cache_workspace_bytes(const lq_cache* host_cache, int32_t n_seqs);
+
+/* Pages for add[i] >= 0 more positions of slot slots[i], i = 0 .. n_seqs - 1: the lowest-numbered free pages, in the order of
+ * (i, position), go to the table, their refs become 1, and lens[slots[i]] grows by add[i].  If the free pages do not
+ * suffice, the first entries whose pages all fit are served, the others are left as they are, and bit 2 is set.  A slot
+ * that the call lists again, or a length beyond max_pages * page_tokens, is skipped (bit 0). */
+lq_status lora_cache_reserve(const lq_cache* host_cache, const int32_t* slots, const int32_t* add, int32_t n_seqs,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
+/* Slot dst_slots[i] (empty, and listed once) becomes a copy of the first keep[i] positions of slot src_slots[i] (keep NULL: of
+ * all of them), as they are when the call begins.  Full pages are shared (refs + 1); a partly filled last page is copied, in all
+ * n_pools pools, into the lowest-numbered free page (in the order of i), so that both sequences can be continued.  pools: device
+ * array of n_pools device pointers, one pool per layer.  Entries are served or left as by lora_cache_reserve.  (A sequence
+ * is cut short by a fork with keep and a free of the old slot.) */
+lq_status lora_cache_fork(const lq_cache* host_cache, const int32_t* src_slots, const int32_t* dst_slots, const int32_t* keep,
+                          int32_t n_seqs, void* const* pools, int32_t n_pools, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The slots become empty: their pages' refs fall by one, their table entries become -1 and their lengths 0. */
+lq_status lora_cache_free(const lq_cache* host_cache, const int32_t* slots, int32_t n_seqs, void* workspace, size_t workspace_bytes,
+                          void* stream);
+
+/* The pages in use become pages 0 .. n_live - 1: the i-th one (by number) of those with numbers from n_live on moves to the i-th
+ * free number below, in all pools; the tables of all slots and refs follow.  n_live int32[1] (device), may be NULL. */
+lq_status lora_cache_compact(const lq_cache* host_cache, void* const* pools, int32_t n_pools, int32_t* n_live, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/* Keys and values of a step's rows into the pages of one layer (`pages`).  k, v  bf16 [n_rows, n_kv_heads * head_dim], leading dimensions
+ * ldk, ldv (multiples of 8, 16-byte aligned).  Per block and head, K and V each: e is the least integer with max |x| <= 448 * 2^e over
+ * the block's new finite elements, within [-100, 119], and not below the block's exponent if the block holds positions before the
+ * span's first (their codes are then brought to the new exponent); code = x * 2^-e rounded to nearest even e4m3, at most
+ * +-448; NaN and infinities become NaN.  Sequences are stored in order: what a block held behind the span's last row is lost.
+ * Only pages with refs == 1 are stored to (bit 0 otherwise); a slot may not be in two spans of a call. */
+lq_status lora_cache_store_rows(const void* k, int64_t ldk, const void* v, int64_t ldv, int32_t n_rows, const lq_cache* host_cache,
+                                void* pages, const int32_t* slots, const int32_t* row_starts, const int32_t* first, int32_t n_seqs,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
+/* The way back, for attention implementations of the caller's own: k, v [n_rows, n_kv_heads * head_dim] bf16 = the values of the
+ * spans' positions (exact). */
+lq_status lora_cache_load_rows(void* k, int64_t ldk, void* v, int64_t ldv, int32_t n_rows, const lq_cache* host_cache, const void* pages,
+                               const int32_t* slots, const int32_t* row_starts, const int32_t* first, int32_t n_seqs,
+                               void* workspace, size_t workspace_bytes, void* stream);
+
+/* Attention of the spans' rows over their sequences' cached positions:
+ *     out[t, h, :] = sum_j p_j V[j, h / G, :],   p = softmax_j(scale * q[t, h, :] . K[j, h / G, :]),   j = 0 .. position of t
+ *   q, out   bf16 [n_rows, n_heads * head_dim], leading dimensions ldq, ldo; n_heads a multiple G of n_kv_heads, up to
+ *            LQ_CACHE_MAX_HEADS; out may not alias q.  Sums and softmax in fp32, p rounded to bf16 for the product with V.
+ *   max_rows the largest number of rows of a span (a bound from above will do): picks the kernel's tile, no result depends on
+ *            it but for the order of sums
+ *   A position that a row does not see leaves no trace in it (NaN included); a row that sees no usable page is zero.
+ *   n_seqs up to LQ_CACHE_MAX_SEQS.  Results are the same from run to run. */
+#define LQ_CACHE_MAX_SEQS 4096
+
+size_t lora_cache_attention_workspace_bytes(const lq_cache* host_cache, int32_t n_heads, int32_t max_rows);
+
+lq_status lora_cache_attention(const void* q, int64_t ldq, void* out, int64_t ldo, int32_t n_rows, int32_t n_heads, float scale,
+                               const lq_cache* host_cache, const void* pages, const int32_t* slots, const int32_t* row_starts,
+                               const int32_t* first, int32_t n_seqs, int32_t max_rows, void* workspace, size_t workspace_bytes,
+                               void* stream);
 
 /* ---------------------------------------------------------------------------------------------
  * Timing of the library's own kernel launches, for benchmarks (not part of the paper's method).

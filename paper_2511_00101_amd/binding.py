@@ -20,6 +20,7 @@ LQ_VARIANT_SPLIT, LQ_VARIANT_FUSED, LQ_VARIANT_SHRINK_ONLY, LQ_VARIANT_EXPAND_ON
 LQ_MAX_RANK = 128
 LQ_MAX_GROUP = 4
 LQ_STATIC_WORKSPACE_BYTES = 4096 + (32 << 20)
+LQ_CACHE_BLOCK, LQ_CACHE_MAX_HEADS, LQ_CACHE_MAX_SEQS, LQ_CACHE_MIN_WORKSPACE = 16, 256, 4096, 4096
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "liblqlora.so")
 _lib = None
@@ -47,6 +48,17 @@ _SIGNATURES = {
     "lora_kind_offsets": (ctypes.c_int, [_vp, _vp, _vp, _i32, _vp, _vp]),
     "lora_split_rows": (ctypes.c_int, [_vp, _i64, _i32, _vp, _i32, _vp, _vp, _i32, _vp, _vp]),
     "lora_concat_rows": (ctypes.c_int, [_vp, _i32, _vp, _i32, _vp, _vp, _i32, _vp, _i64, _vp]),
+    "lora_cache_page_bytes": (_sz, [_i32, _i32, _i32]),
+    "lora_cache_workspace_bytes": (_sz, [_vp, _i32]),
+    "lora_cache_reserve": (ctypes.c_int, [_vp, _vp, _vp, _i32, _vp, _sz, _vp]),
+    "lora_cache_fork": (ctypes.c_int, [_vp, _vp, _vp, _vp, _i32, _vp, _i32, _vp, _sz, _vp]),
+    "lora_cache_free": (ctypes.c_int, [_vp, _vp, _i32, _vp, _sz, _vp]),
+    "lora_cache_compact": (ctypes.c_int, [_vp, _vp, _i32, _vp, _vp, _sz, _vp]),
+    "lora_cache_store_rows": (ctypes.c_int, [_vp, _i64, _vp, _i64, _i32, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _sz, _vp]),
+    "lora_cache_load_rows": (ctypes.c_int, [_vp, _i64, _vp, _i64, _i32, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _sz, _vp]),
+    "lora_cache_attention_workspace_bytes": (_sz, [_vp, _i32, _i32]),
+    "lora_cache_attention": (ctypes.c_int, [_vp, _i64, _vp, _i64, _i32, _i32, ctypes.c_float, _vp, _vp, _vp, _vp, _vp, _i32, _i32,
+                                            _vp, _sz, _vp]),
     "lora_profile_enable": (ctypes.c_int, [_i32]),
     "lora_profile_read": (ctypes.c_int, [_vp, _vp, _i32]),
 }
@@ -370,6 +382,156 @@ def lora_concat_rows(parts: torch.Tensor, seg: SegmentTables, dst: torch.Tensor,
         raise LqError(st, "lora_concat_rows")
 
 
+# ---- paged 8-bit key/value cache ----------------------------------------------------------------------------------
+class _CacheStruct(ctypes.Structure):
+    _fields_ = [(n, _i32) for n in ("n_kv_heads", "head_dim", "page_tokens", "n_pages", "n_slots", "max_pages")] + [
+        (n, _vp) for n in ("table", "lens", "refs")]
+
+
+class PagedCache:
+    """The tensors of a paged key/value cache and the host block that describes them to the library.
+
+    pages: one uint8 tensor [n_pages, page bytes] per layer; table int32[n_slots, max_pages], lens int32[n_slots], refs
+    int32[n_pages].  Takes the tensors as they are (`empty` allocates an empty cache)."""
+
+    def __init__(self, n_kv_heads: int, head_dim: int, page_tokens: int, pages: Sequence[torch.Tensor], table: torch.Tensor,
+                 lens: torch.Tensor, refs: torch.Tensor):
+        assert all(t.dtype == torch.int32 and t.is_contiguous() for t in (table, lens, refs))
+        assert table.dim() == 2 and lens.numel() == table.shape[0]
+        n_bytes = lora_cache_page_bytes(n_kv_heads, head_dim, page_tokens)
+        for p in pages:
+            assert p.dtype == torch.uint8 and p.is_contiguous() and tuple(p.shape) == (refs.numel(), n_bytes)
+        self.n_kv_heads, self.head_dim, self.page_tokens = n_kv_heads, head_dim, page_tokens
+        self.pages, self.table, self.lens, self.refs = list(pages), table, lens, refs
+        self.pools = torch.tensor([p.data_ptr() for p in pages], dtype=torch.int64, device=refs.device)
+        self.struct = _CacheStruct(n_kv_heads, head_dim, page_tokens, refs.numel(), table.shape[0], table.shape[1],
+                                   table.data_ptr(), lens.data_ptr(), refs.data_ptr())
+        self.ref = ctypes.addressof(self.struct)
+
+    @staticmethod
+    def empty(n_layers: int, n_kv_heads: int, head_dim: int, page_tokens: int, n_pages: int, n_slots: int, max_pages: int,
+              device="cuda") -> "PagedCache":
+        n_bytes = lora_cache_page_bytes(n_kv_heads, head_dim, page_tokens)
+        if not n_bytes:
+            raise LqError(LQ_ERR_UNSUPPORTED, "PagedCache.empty")
+        dev = torch.device(device)
+        return PagedCache(n_kv_heads, head_dim, page_tokens,
+                          [torch.zeros(n_pages, n_bytes, dtype=torch.uint8, device=dev) for _ in range(n_layers)],
+                          torch.full((n_slots, max_pages), -1, dtype=torch.int32, device=dev),
+                          torch.zeros(n_slots, dtype=torch.int32, device=dev), torch.zeros(n_pages, dtype=torch.int32, device=dev))
+
+
+def lora_cache_page_bytes(n_kv_heads: int, head_dim: int, page_tokens: int) -> int:
+    return int(lib().lora_cache_page_bytes(n_kv_heads, head_dim, page_tokens))
+
+
+def lora_cache_workspace_bytes(cache: PagedCache, n_seqs: int) -> int:
+    return int(lib().lora_cache_workspace_bytes(cache.ref, n_seqs))
+
+
+def lora_cache_attention_workspace_bytes(cache: PagedCache, n_heads: int, max_rows: int) -> int:
+    return int(lib().lora_cache_attention_workspace_bytes(cache.ref, n_heads, max_rows))
+
+
+def _index(t: Optional[torch.Tensor], n: int) -> Optional[int]:
+    if t is None:
+        return None
+    assert t.dtype == torch.int32 and t.is_contiguous() and t.numel() == n
+    return t.data_ptr()
+
+
+def _workspace_args(workspace):
+    return _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def lora_cache_reserve(cache: PagedCache, slots: torch.Tensor, add: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
+    """Pages for add[i] more positions of slot slots[i]."""
+    n = slots.numel()
+    st = lib().lora_cache_reserve(cache.ref, _index(slots, n), _index(add, n), n, *_workspace_args(workspace), _stream(stream))
+    if st != LQ_OK:
+        raise LqError(st, "lora_cache_reserve")
+
+
+def lora_cache_fork(cache: PagedCache, src_slots: torch.Tensor, dst_slots: torch.Tensor, workspace: torch.Tensor,
+                    keep: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Slots dst_slots become copies of (the first `keep` positions of) slots src_slots, in all layers."""
+    n = src_slots.numel()
+    st = lib().lora_cache_fork(cache.ref, _index(src_slots, n), _index(dst_slots, n), _index(keep, n), n, _ptr(cache.pools), len(cache.pages),
+                               *_workspace_args(workspace), _stream(stream))
+    if st != LQ_OK:
+        raise LqError(st, "lora_cache_fork")
+
+
+def lora_cache_free(cache: PagedCache, slots: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
+    n = slots.numel()
+    st = lib().lora_cache_free(cache.ref, _index(slots, n), n, *_workspace_args(workspace), _stream(stream))
+    if st != LQ_OK:
+        raise LqError(st, "lora_cache_free")
+
+
+def lora_cache_compact(cache: PagedCache, n_live: Optional[torch.Tensor], workspace: torch.Tensor, stream=None) -> None:
+    """Live pages move to the lowest numbers; n_live int32[1] (or None) receives how many there are."""
+    st = lib().lora_cache_compact(cache.ref, _ptr(cache.pools), len(cache.pages), _index(n_live, 1), *_workspace_args(workspace),
+                                  _stream(stream))
+    if st != LQ_OK:
+        raise LqError(st, "lora_cache_compact")
+
+
+def _span_args(cache, layer, slots, row_starts, first):
+    n = first.numel()
+    return cache.ref, _ptr(cache.pages[layer]), _index(slots, n), _index(row_starts, n + 1), _index(first, n), n
+
+
+def _cache_rows_args(k, v, cache, layer, slots, row_starts, first, workspace, stream):
+    assert k.dtype == torch.bfloat16 and v.dtype == torch.bfloat16 and k.stride(1) == 1 and v.stride(1) == 1
+    assert k.shape == v.shape and k.shape[1] == cache.n_kv_heads * cache.head_dim
+    n_rows = int(k.shape[0])
+    return (_ptr(k), k.stride(0), _ptr(v), v.stride(0), n_rows, *_span_args(cache, layer, slots, row_starts, first),
+            *_workspace_args(workspace), _stream(stream))
+
+
+def lora_cache_store_rows(k: torch.Tensor, v: torch.Tensor, cache: PagedCache, layer: int, slots: Optional[torch.Tensor],
+                          row_starts: torch.Tensor, first: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
+    """Rows row_starts[s] .. of k and v into positions first[s] .. of slot slots[s] (quantised), in one layer's pages."""
+    st = lib().lora_cache_store_rows(*_cache_rows_args(k, v, cache, layer, slots, row_starts, first, workspace, stream))
+    if st != LQ_OK:
+        raise LqError(st, "lora_cache_store_rows")
+
+
+def lora_cache_load_rows(k: torch.Tensor, v: torch.Tensor, cache: PagedCache, layer: int, slots: Optional[torch.Tensor],
+                         row_starts: torch.Tensor, first: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
+    """The way back: k and v receive the cached values as bf16."""
+    st = lib().lora_cache_load_rows(*_cache_rows_args(k, v, cache, layer, slots, row_starts, first, workspace, stream))
+    if st != LQ_OK:
+        raise LqError(st, "lora_cache_load_rows")
+
+
+def _attention_args(q, out, cache, layer, slots, row_starts, first, max_rows, workspace, scale, stream):
+    assert q.dtype == torch.bfloat16 and out.dtype == torch.bfloat16 and q.stride(1) == 1 and out.stride(1) == 1
+    assert q.shape == out.shape and q.shape[1] % cache.head_dim == 0
+    scale = cache.head_dim ** -0.5 if scale is None else float(scale)
+    return (_ptr(q), q.stride(0), _ptr(out), out.stride(0), int(q.shape[0]), int(q.shape[1]) // cache.head_dim, scale,
+            *_span_args(cache, layer, slots, row_starts, first), int(max_rows), *_workspace_args(workspace), _stream(stream))
+
+
+def lora_cache_attention(q: torch.Tensor, out: torch.Tensor, cache: PagedCache, layer: int, slots: Optional[torch.Tensor],
+                         row_starts: torch.Tensor, first: torch.Tensor, max_rows: int, workspace: torch.Tensor,
+                         scale: Optional[float] = None, stream=None) -> None:
+    """Attention of the spans' rows (q, out: [rows, heads * head_dim]) over their slots' cached positions up to their own.
+    max_rows: the longest span's rows, or a bound; scale: head_dim ** -0.5 unless given."""
+    st = lib().lora_cache_attention(*_attention_args(q, out, cache, layer, slots, row_starts, first, max_rows, workspace, scale, stream))
+    if st != LQ_OK:
+        raise LqError(st, "lora_cache_attention")
+
+
+def prepare_cache_attention(q, out, cache, layer, slots, row_starts, first, max_rows, workspace, scale=None, stream=None) -> PreparedCall:
+    call = PreparedCall(lib().lora_cache_attention,
+                        _attention_args(q, out, cache, layer, slots, row_starts, first, max_rows, workspace, scale, stream),
+                        "lora_cache_attention")
+    call.keep = cache      # the host block that the arguments point to
+    return call
+
+
 # ---- plumbing between numpy bf16 bit patterns and device tensors ------------------------------------------------
 def bf16_from_bits(bits: np.ndarray, device="cuda") -> torch.Tensor:
     return torch.from_numpy(np.ascontiguousarray(bits).view(np.int16)).view(torch.bfloat16).to(device)
@@ -384,6 +546,7 @@ def workspace(n_bytes: int, device="cuda") -> torch.Tensor:
 
 
 LQ_DEVICE_ERR_BAD_SEGMENT = 1      # a segment was skipped: adapter id, rank, matrix pointer or row range unusable
+LQ_DEVICE_ERR_NO_PAGES = 4         # the cache's free pages ran out: the last entries of a reserve or fork were left as they are
 LQ_DEVICE_ERR_BARRIER_TIMEOUT = 2  # the single-launch kernel's device-wide wait ran out: y / dx were left untouched
 
 
@@ -392,6 +555,7 @@ class LqDeviceError(RuntimeError):
 
     def __init__(self, bits: int, where: str):
         names = [n for b, n in ((LQ_DEVICE_ERR_BAD_SEGMENT, "bad segment table entry (segment skipped)"),
+                                (LQ_DEVICE_ERR_NO_PAGES, "no free pages left (the last entries were not served)"),
                                 (LQ_DEVICE_ERR_BARRIER_TIMEOUT, "device-wide wait timed out (outputs left untouched; "
                                  "use LQ_VARIANT_SLAB or LQ_VARIANT_SPLIT when the device is shared)")) if bits & b]
         super().__init__(f"{where}: device error word {bits:#x}: " + "; ".join(names or ["unknown bits"]))
