@@ -423,8 +423,9 @@ lq_status lora_cache_load_rows(void* k, int64_t ldk, void* v, int64_t ldv, int32
  *   max_rows the largest number of rows of a span (a bound from above will do): picks the kernel's tile, no result depends on
  *            it but for the order of sums
  *   A position that a row does not see leaves no trace in it (NaN included); a row that sees no usable page is zero.
- *   n_seqs up to LQ_CACHE_MAX_SEQS.  Results are the same from run to run. */
+ *   n_seqs up to LQ_CACHE_MAX_SEQS, n_rows up to LQ_CACHE_MAX_ROWS.  Results are the same from run to run. */
 #define LQ_CACHE_MAX_SEQS 4096
+#define LQ_CACHE_MAX_ROWS (1 << 22)
 
 size_t lora_cache_attention_workspace_bytes(const lq_cache* host_cache, int32_t n_heads, int32_t max_rows);
 

@@ -1,9 +1,37 @@
-// Attention of a step's rows over the paged 8-bit cache.
+// Attention of a step's rows over the paged 8-bit cache: single tokens, drafts and prompts by one kernel.
+//
+// Mathematics: a row's probabilities are 2^(c s_j - m), c = scale log2(e), with a maximum m that only follows when a score exceeds it by
+// more than 8 (in log2), so one pass over the positions suffices and the sums are rescaled rarely; any m gives the same quotient.
+//
+// Tiles: 16 x NT rows (token-major: row = token * G + query head of the group) stand as the columns of S^T = K Q^T, so the accumulator
+// layout of S^T (lane: one row; registers: keys 4 kg + r of a block of 16) IS the B operand layout of O^T = V^T P^T as far as the
+// order of the keys inside the k dimension goes, which is free: P never leaves its registers.  K's codes are loaded in the A operand
+// layout directly (16 bytes = the lane's share of two k steps), V's layout in the page gives a lane four positions of a
+// column in one word.  The codes become bf16 in registers (v_cvt_scalef32: the block's scale costs nothing), so neither K nor V passes
+// through LDS.  The four waves of a workgroup take alternate 32-key steps with maxima of their own and are added at the end.
+//
+// Work: units of (span, row tile, key head, chunk of positions).  Every workgroup works the unit list out from the spans (a prefix
+// sum), so no plan is launched or kept; the chunk length is the batch's total work over the partial sums' slots, so that long
+// sequences are split where there are few rows and not where there are many.  The last chunk of a tile to arrive adds the tile's
+// partial sums in chunk order.
 #include "lq_cache.h"
 #include "lq_internal.h"
 
 namespace lq {
 namespace {
+
+constexpr int kAttnThreads = 256, kAttnWaves = kAttnThreads / kWave;
+constexpr int kStep = 32;                       // keys of a wave's step: two blocks
+constexpr int kRound = kStep * kAttnWaves;      // keys of a workgroup's round
+constexpr int kMaxChunks = 255;                 // arrivals are counted in a byte
+// Bytes of the workspace header that count the arrivals at split tiles: behind the barrier's words (kBarSub and its lines).
+constexpr int kArrivals = kBarSub + kBarFan * kBarLine;
+constexpr int kArrivalBytes = kWsHeaderBytes - 4 * kArrivals;
+// Partial-sum slots: a split tile has at least two, and its counter is its first slot's index / 2.
+template <int NT> constexpr int kSlots = NT == 1 ? 2 * kArrivalBytes : NT == 2 ? 2048 : 1024;
+static_assert(kSlots<1> / 2 <= kArrivalBytes && kSlots<2> / 2 <= kArrivalBytes && kSlots<4> / 2 <= kArrivalBytes, "a byte per split tile");
+constexpr float kLazy = 8.f;                    // log2 of how far a score may exceed the maximum that its exponentials use
+constexpr int kRawBuffer = 0x00020000, kSc1 = 16;   // descriptor word 3 (raw 32-bit data); device-scope cache policy
 
 struct AttnParams {
     CacheView c;
@@ -12,80 +40,527 @@ struct AttnParams {
     u16* out; long long ldo;
     const uint8_t* pages;
     int n_heads, group;
-    float scale;
+    float c_log2;               // |scale| * log2(e)
+    unsigned int q_sign;        // 0x80008000 where the scale is negative
+    float* partial;
+    unsigned int partial_bytes;
+    int* tickets;
+    uint8_t* arrivals;
 };
 
-// One wave per (row, head): lanes over 64 positions for the scores, over the columns for the sum.
+template <int HD, int NT> constexpr int slot_floats() { return 16 * NT * (HD + 2); }
+
+// codes of a step: per block of 16 keys K in the A operand layout, V in words of four positions, and the two exponent bytes
 template <int HD>
-__global__ __launch_bounds__(64) void attention_kernel(AttnParams p)
+struct Step {
+    u32x4 k[2][HD / 64], v[2][HD / 64];
+    unsigned int e[2];
+    bool ok[2];                 // wave uniform: the block is there
+};
+
+__device__ __forceinline__ unsigned int to_bf16(unsigned int w, float scale, bool high)
 {
-    __shared__ float qs[HD], ps[kWave];
-    const CacheView& c = p.c;
-    const int lane = lane_id();
-    const int row = (int)(blockIdx.x / p.n_heads), head = (int)(blockIdx.x % p.n_heads), kvh = head / p.group;
-    const int s = last_not_above(p.sp.n_seqs, row, [&](int k) { return p.sp.row_starts[k]; });
-    if (s < 0) return;
-    const Span u = load_span(c, p.sp, s);
-    if (row - u.row0 >= u.n) return;
-    const int pos = u.first + row - u.row0;
-    const int T = 1 << c.t_log2;
-    const u16* qr = p.q + row * p.ldq + head * HD;
+    return __builtin_bit_cast(unsigned int, high ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true)
+                                                 : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false));
+}
+__device__ __forceinline__ bf16x8 eight_bf16(unsigned int a, float sa, unsigned int b, float sb)
+{
+    return __builtin_bit_cast(bf16x8, u32x4{to_bf16(a, sa, false), to_bf16(a, sa, true), to_bf16(b, sb, false), to_bf16(b, sb, true)});
+}
+__device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+// maximum (sum) over the four lanes that hold one column
+__device__ __forceinline__ float column_max(float v)
+{
+    typedef __attribute__((ext_vector_type(2))) unsigned int pair;
+    const unsigned int u = __float_as_uint(v);
+    const pair a = __builtin_bit_cast(pair, __builtin_amdgcn_permlane16_swap(u, u, false, false));
+    const unsigned int w = __float_as_uint(fmaxf(__uint_as_float(a.x), __uint_as_float(a.y)));
+    const pair b = __builtin_bit_cast(pair, __builtin_amdgcn_permlane32_swap(w, w, false, false));
+    return fmaxf(__uint_as_float(b.x), __uint_as_float(b.y));
+}
+__device__ __forceinline__ float column_sum(float v)
+{
+    v += __shfl_xor(v, 16, kWave);
+    return v + __shfl_xor(v, 32, kWave);
+}
+
+// page numbers of a slot's row, 64 entries in the lanes and the next 64 behind them
+struct PageIds {
+    const int32_t* row;
+    int held, batch;
+    int now, next;
+    __device__ __forceinline__ int load(int b) const { return row[min(b * kWave + lane_id(), held - 1)]; }
+    __device__ __forceinline__ void start(const int32_t* r, int n, int entry)
+    {
+        row = r;
+        held = n;
+        batch = entry / kWave;
+        now = load(batch);
+        next = load(batch + 1);
+    }
+    __device__ __forceinline__ int get(int entry)
+    {
+        if (entry / kWave != batch) {   // wave uniform; entries are asked for in order
+            now = next;
+            batch = entry / kWave;
+            next = load(batch + 1);
+        }
+        return lane_value(now, entry % kWave);
+    }
+};
+
+struct Unit { int slot, row0, n, first, tile, head, chunk, chunks, slot0; };   // slot0: first partial-sum slot of the tile
+
+template <int HD, int NT>
+struct Attention {
+    static constexpr int D = HD / 16;           // O^T rows of a lane's accumulator register set; also V words of a lane and block
+    static constexpr int LD = HD / 64;          // 16-byte loads of a lane for 16 keys
+    static constexpr int PITCH = HD + 4;
+    struct Shared {
+        float acc[kAttnWaves][16][PITCH];
+        float m[kAttnWaves][16 * NT], l[kAttnWaves][16 * NT];
+        long long sums[kAttnWaves];
+        int slot[2], last, total, chunk_len;
+    };
+
+    static __device__ __forceinline__ void load_step(const AttnParams& p, PageIds& ids, const Unit& u, int key0, int last_key, Step<HD>& s)
+    {
+        const CacheView& c = p.c;
+        const int T = 1 << c.t_log2, lane = lane_id();
 #pragma unroll
-    for (int d = lane; d < HD; d += kWave) qs[d] = __uint_as_float((unsigned)qr[d] << 16) * p.scale;
-    __syncthreads();
-    float mx = -__builtin_inff(), sum = 0.f, o[HD / kWave] = {};
-    const int32_t* table = c.table + (long long)u.slot * c.max_pages;
-    for (int j0 = 0; j0 <= pos; j0 += kWave) {
-        const int j = j0 + lane;
-        float sc = -__builtin_inff();
-        if (j <= pos) {
-            const int page = table[j >> c.t_log2];
-            if (page < 0 || page >= c.n_pages) atomicOr(c.err, kErrBadSegment);
-            else {
-                const uint8_t* pg = p.pages + page * c.page_bytes;
-                const int in = j & (T - 1);
-                const unsigned int* kc = reinterpret_cast<const unsigned int*>(pg + (long long)kvh * 2 * T * HD + in * HD);
-                const float ks = block_scale(pg[c.scale_off + (kvh * (T / kBlock) + in / kBlock) * 2]);
-                sc = 0.f;
-                for (int i = 0; i < HD / 4; ++i) {
-                    const unsigned int w = kc[i];
-                    const unsigned int lo = __builtin_bit_cast(unsigned int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, ks, false));
-                    const unsigned int hi = __builtin_bit_cast(unsigned int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, ks, true));
-                    sc += qs[4 * i] * bf16_lo(lo) + qs[4 * i + 1] * bf16_hi(lo) + qs[4 * i + 2] * bf16_lo(hi) + qs[4 * i + 3] * bf16_hi(hi);
+        for (int b = 0; b < 2; ++b) {
+            const int key = key0 + b * kBlock;
+            const bool wanted = key <= last_key;
+            const int page = wanted ? ids.get(key >> c.t_log2) : -1;
+            const bool ok = page >= 0 && page < c.n_pages;
+            if (wanted && !ok && lane == 0) atomicOr(c.err, kErrBadSegment);
+            // a block that is not there reads as zeros
+            const uint8_t* at = p.pages + (ok ? page : 0) * c.page_bytes;
+            const __amdgpu_buffer_rsrc_t page_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(at), 0, ok ? (int)c.page_bytes : 0, kRawBuffer);
+            const int in = key & (T - 1);
+            const int k_off = u.head * 2 * T * HD + in * HD, v_off = k_off + T * HD;
+            s.e[b] = __builtin_amdgcn_raw_buffer_load_b16(page_rsrc, 0, c.scale_off + (u.head * (T / kBlock) + in / kBlock) * 2, 0);
+#pragma unroll
+            for (int j = 0; j < LD; ++j)
+                s.k[b][j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(page_rsrc, (lane & 15) * HD + (lane >> 4) * 16 + 64 * j, k_off, 0));
+#pragma unroll
+            for (int j = 0; j < LD; ++j)
+                s.v[b][j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(page_rsrc, (lane >> 4) * 4 * HD + (lane & 15) * 4 * D + 16 * j, v_off, 0));
+            s.ok[b] = ok;
+        }
+    }
+
+    // One unit's chunk: the wave's share of the positions [begin, end).
+    struct State { f32x4 o[NT][D]; float m[NT], l[NT]; };
+
+    static __device__ __forceinline__ void one_step(const Step<HD>& s, const bf16x8 (&q)[NT][HD / 32], const int (&limit)[NT], int key0, int last_key,
+                                                    bool masked, float c_log2, State& st)
+    {
+        const int kg = lane_id() >> 4;
+        f32x4 sc[2][NT];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const float ks = block_scale(s.e[b] & 0xffu);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) sc[b][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < LD; ++j)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const bf16x8 a = h == 0 ? eight_bf16(s.k[b][j].x, ks, s.k[b][j].y, ks) : eight_bf16(s.k[b][j].z, ks, s.k[b][j].w, ks);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) sc[b][n] = mfma(a, q[n][2 * j + h], sc[b][n]);
+                }
+        }
+        unsigned int vw[2][D];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < D; ++i) vw[b][i] = s.v[b][i / 4][i % 4];
+        if (masked) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const int key = key0 + b * kBlock + 4 * kg;
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (!s.ok[b] || key + r > limit[n]) sc[b][n][r] = -__builtin_inff();
+                // what lies in the page behind the last position that any row sees is nobody's
+                const int live = last_key + 1 - key;
+                const unsigned int keep = live >= 4 ? ~0u : live <= 0 ? 0u : (1u << (8 * live)) - 1u;
+#pragma unroll
+                for (int i = 0; i < D; ++i) vw[b][i] &= keep;
+            }
+        }
+        bf16x8 pt[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            float t = sc[0][n][0];
+#pragma unroll
+            for (int r = 1; r < 8; ++r) t = fmaxf(t, sc[r / 4][n][r % 4]);
+            t = column_max(t) * c_log2;
+            if (__any(t > st.m[n] + kLazy)) {
+                const float m = fmaxf(st.m[n], t);
+                const float a = m == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(st.m[n] - m);
+                st.m[n] = m;
+                st.l[n] *= a;
+#pragma unroll
+                for (int i = 0; i < D; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) st.o[n][i][r] *= a;
+            }
+            const float m = st.m[n] == -__builtin_inff() ? 0.f : st.m[n];   // (nothing seen yet: 2^-inf = 0)
+            float e[8], sum = 0.f;
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                e[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[r / 4][n][r % 4], c_log2, -m));
+                sum += e[r];
+            }
+            st.l[n] += sum;
+            // bf16 probabilities (rounded: 2^-9 of a term on average in the sum of p v, below the output's own rounding)
+            pt[n] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7])});
+        }
+        if (masked) {
+            // 0 x NaN is NaN: a NaN value must reach the rows that see its position and no others
+            unsigned int nan = 0;
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < D; ++i) nan |= ((vw[b][i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+            if (__any(nan != 0)) {
+                unsigned int seen[NT][4];
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int key = key0 + (r / 2) * kBlock + 4 * kg + 2 * (r % 2);
+                        seen[n][r] = (s.ok[r / 2] && key <= limit[n] ? 0x3f80u : 0u) | (s.ok[r / 2] && key + 1 <= limit[n] ? 0x3f800000u : 0u);
+                    }
+#pragma unroll
+                for (int i = 0; i < D; ++i) {
+                    unsigned int one[2];
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        const unsigned int bad = (((vw[b][i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7;   // 1 per NaN byte
+                        one[b] = bad * 0x38u;                                                                      // e4m3 1.0
+                        vw[b][i] &= ~(bad * 0xffu);
+                    }
+                    const bf16x8 a = eight_bf16(one[0], 1.f, one[1], 1.f);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        const f32x4 hit = mfma(a, __builtin_bit_cast(bf16x8, u32x4{seen[n][0], seen[n][1], seen[n][2], seen[n][3]}), f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (hit[r] > 0.f) st.o[n][i][r] = __builtin_nanf("");
+                    }
                 }
             }
         }
-        float m = sc;
+        const float v0 = block_scale(s.e[0] >> 8), v1 = block_scale(s.e[1] >> 8);
 #pragma unroll
-        for (int d = 1; d < kWave; d <<= 1) m = fmaxf(m, __shfl_xor(m, d, kWave));
-        m = fmaxf(m, mx);
-        if (m == -__builtin_inff()) m = 0.f;                       // nothing seen so far
-        const float a = __expf(mx - m), e = sc == -__builtin_inff() ? 0.f : __expf(sc - m);
-        mx = m;
-        ps[lane] = e;
-        float t = e;
+        for (int i = 0; i < D; ++i) {
+            const bf16x8 a = eight_bf16(vw[0][i], v0, vw[1][i], v1);
 #pragma unroll
-        for (int d = 1; d < kWave; d <<= 1) t += __shfl_xor(t, d, kWave);
-        sum = sum * a + t;
-        __syncthreads();
-        for (int i = 0; i < HD / kWave; ++i) {
-            const int d = lane + i * kWave;
-            float acc = o[i] * a;
-            for (int k = 0; k < kWave && j0 + k <= pos; ++k) {
-                const int page = table[(j0 + k) >> c.t_log2];
-                if (page < 0 || page >= c.n_pages) continue;
-                const uint8_t* pg = p.pages + page * c.page_bytes;
-                const int in = (j0 + k) & (T - 1);
-                const float vs = block_scale(pg[c.scale_off + (kvh * (T / kBlock) + in / kBlock) * 2 + 1]);
-                const unsigned int w = pg[(long long)(kvh * 2 + 1) * T * HD + (in >> 2) * 4 * HD + 4 * d + (in & 3)];
-                acc += ps[k] * bf16_lo(__builtin_bit_cast(unsigned int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, vs, false)));
+            for (int n = 0; n < NT; ++n) st.o[n][i] = mfma(a, pt[n], st.o[n][i]);
+        }
+    }
+
+    static __device__ __forceinline__ void run_unit(const AttnParams& p, const Unit& u, int chunk_len, Shared& sh)
+    {
+        const CacheView& c = p.c;
+        const int lane = lane_id(), wave = uniform((int)threadIdx.x / kWave), col = lane & 15, kg = lane >> 4;
+        const int rows = u.n * p.group, row_base = u.tile * 16 * NT;
+        const int last_row = min(row_base + 16 * NT, rows) - 1;
+        const int last_key = u.first + last_row / p.group;                        // the last position that a row of the tile sees
+        const int begin = u.chunk * chunk_len, end = min(begin + chunk_len, last_key + 1);
+        const int first_pos = u.first + row_base / p.group;                       // the first row's
+
+        bf16x8 q[NT][HD / 32];
+        int limit[NT];
+        State st;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int r = row_base + 16 * n + col;
+            const int token = r / p.group, h = u.head * p.group + r % p.group;
+            limit[n] = r < rows ? u.first + token : -1;
+            const u16* src = p.q + (long long)(u.row0 + token) * p.ldq + h * HD + kg * 16;
+#pragma unroll
+            for (int j = 0; j < HD / 32; ++j) {
+                u32x4 w{0, 0, 0, 0};
+                if (r < rows) w = *reinterpret_cast<const u32x4*>(src + (j / 2) * 64 + (j % 2) * 8);
+                w.x ^= p.q_sign; w.y ^= p.q_sign; w.z ^= p.q_sign; w.w ^= p.q_sign;
+                q[n][j] = __builtin_bit_cast(bf16x8, w);
             }
-            o[i] = acc;
+            st.m[n] = -__builtin_inff();
+            st.l[n] = 0.f;
+#pragma unroll
+            for (int i = 0; i < D; ++i) st.o[n][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+
+        int key = begin + wave * kStep;
+        if (key < end) {
+            PageIds ids;
+            ids.start(c.table + (long long)u.slot * c.max_pages, (last_key >> c.t_log2) + 1, key >> c.t_log2);
+            Step<HD> s;
+            load_step(p, ids, u, key, last_key, s);
+            while (true) {
+                const int next = key + kRound;
+                Step<HD> ahead = s;
+                if (next < end) load_step(p, ids, u, next, last_key, ahead);
+                const bool masked = key + kStep - 1 > first_pos || !s.ok[0] || !s.ok[1];
+                one_step(s, q, limit, key, last_key, masked, p.c_log2, st);
+                if (next >= end) break;
+                key = next;
+                s = ahead;
+            }
+        }
+
+        // the waves' maxima and sums
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const float l = column_sum(st.l[n]);
+            if (kg == 0) {
+                sh.m[wave][16 * n + col] = st.m[n];
+                sh.l[wave][16 * n + col] = l;
+            }
         }
         __syncthreads();
+        const bool split = u.chunks > 1;
+        const int out_row = (int)threadIdx.x / 16, out_col = (int)threadIdx.x % 16 * D;
+        const __amdgpu_buffer_rsrc_t part = __builtin_amdgcn_make_buffer_rsrc(p.partial, 0, (int)p.partial_bytes, kRawBuffer);
+        const int slot_bytes = slot_floats<HD, NT>() * 4, stat_at = 16 * NT * HD * 4;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            float top = sh.m[0][16 * n + col];
+#pragma unroll
+            for (int w = 1; w < kAttnWaves; ++w) top = fmaxf(top, sh.m[w][16 * n + col]);
+            const float a = st.m[n] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(st.m[n] - top);
+#pragma unroll
+            for (int i4 = 0; i4 < D / 4; ++i4)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const f32x4 v{st.o[n][4 * i4][r] * a, st.o[n][4 * i4 + 1][r] * a, st.o[n][4 * i4 + 2][r] * a, st.o[n][4 * i4 + 3][r] * a};
+                    *reinterpret_cast<f32x4*>(&sh.acc[wave][col][(4 * kg + r) * D + 4 * i4]) = v;
+                }
+            __syncthreads();
+            const int r = row_base + 16 * n + out_row;
+            if (r < rows) {
+                float mt = sh.m[0][16 * n + out_row], l = 0.f;
+#pragma unroll
+                for (int w = 1; w < kAttnWaves; ++w) mt = fmaxf(mt, sh.m[w][16 * n + out_row]);
+#pragma unroll
+                for (int w = 0; w < kAttnWaves; ++w) {
+                    const float mw = sh.m[w][16 * n + out_row];
+                    l += mw == -__builtin_inff() ? 0.f * sh.l[w][16 * n + out_row] : sh.l[w][16 * n + out_row] * __builtin_amdgcn_exp2f(mw - mt);
+                }
+                float o[D];
+#pragma unroll
+                for (int i = 0; i < D; ++i) {
+                    o[i] = 0.f;
+#pragma unroll
+                    for (int w = 0; w < kAttnWaves; ++w) o[i] += sh.acc[w][out_row][out_col + i];
+                }
+                if (!split) write_out(p, u, r, out_col, o, l);
+                else {
+                    const int at = (u.slot0 + u.chunk) * slot_bytes;
+                    const int row = 16 * n + out_row;
+#pragma unroll
+                    for (int i = 0; i < D; i += 4)
+                        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{o[i], o[i + 1], o[i + 2], o[i + 3]}), part, (row * HD + out_col + i) * 4, at, kSc1);
+                    if (out_col == 0)
+                        __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, f32x2{mt, l}), part, stat_at + row * 8, at, kSc1);
+                }
+            }
+            __syncthreads();
+        }
+        if (!split) return;
+
+        // the last chunk of the tile adds them up
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            const int i = u.slot0 / 2, shift = 8 * (i % 4);
+            int* word = reinterpret_cast<int*>(p.arrivals) + i / 4;
+            const int old = __hip_atomic_fetch_add(word, 1 << shift, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            const bool last = ((old >> shift) & 255) == u.chunks - 1;
+            if (last) __hip_atomic_fetch_sub(word, (int)((unsigned)u.chunks << shift), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            sh.last = last;
+        }
+        __syncthreads();
+        if (!sh.last) return;
+        asm volatile("" ::: "memory");
+        for (int n = 0; n < NT; ++n) {
+            const int row = 16 * n + out_row, r = row_base + row;
+            if (r >= rows) continue;
+            float top = -__builtin_inff();
+            for (int k = 0; k < u.chunks; ++k)
+                top = fmaxf(top, __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(part, stat_at + row * 8, (u.slot0 + k) * slot_bytes, kSc1)));
+            float o[D], l = 0.f;
+#pragma unroll
+            for (int i = 0; i < D; ++i) o[i] = 0.f;
+#pragma unroll 4
+            for (int k = 0; k < u.chunks; ++k) {
+                const int at = (u.slot0 + k) * slot_bytes;
+                const f32x2 ml = __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(part, stat_at + row * 8, at, kSc1));
+                const float a = ml.x == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
+                l += ml.y * a;
+#pragma unroll
+                for (int i = 0; i < D; i += 4) {
+                    const f32x4 v = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(part, (row * HD + out_col + i) * 4, at, kSc1));
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) o[i + x] += v[x] * a;
+                }
+            }
+            write_out(p, u, r, out_col, o, l);
+        }
     }
-    u16* orow = p.out + row * p.ldo + head * HD;
-    for (int i = 0; i < HD / kWave; ++i) orow[lane + i * kWave] = (u16)f32_to_bf16_bits(sum == 0.f ? 0.f : o[i] / sum);
+
+    static __device__ __forceinline__ void write_out(const AttnParams& p, const Unit& u, int r, int col, const float* o, float l)
+    {
+        const int token = r / p.group, h = u.head * p.group + r % p.group;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        unsigned int w[D / 2];
+#pragma unroll
+        for (int i = 0; i < D / 2; ++i) w[i] = pack_bf16x2(o[2 * i] * inv, o[2 * i + 1] * inv);
+        u16* dst = p.out + (long long)(u.row0 + token) * p.ldo + h * HD + col;
+        if constexpr (D == 8) *reinterpret_cast<u32x4*>(dst) = u32x4{w[0], w[1], w[2], w[3]};
+        else *reinterpret_cast<u32x2*>(dst) = u32x2{w[0], w[1]};
+    }
+};
+
+__device__ __forceinline__ long long block_total(long long v, long long* sums)
+{
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) v += __shfl_xor(v, d, kWave);
+    __syncthreads();
+    if (lane_id() == 0) sums[threadIdx.x / kWave] = v;
+    __syncthreads();
+    long long t = 0;
+#pragma unroll
+    for (int w = 0; w < kAttnWaves; ++w) t += sums[w];
+    return t;
+}
+
+template <int HD, int NT>
+__global__ __launch_bounds__(kAttnThreads, NT == 1 ? 3 : 2) void attention_kernel(AttnParams p)
+{
+    using A = Attention<HD, NT>;
+    __shared__ typename A::Shared sh;
+    extern __shared__ int prefix[];             // per span: units before it; and partial-sum slots before it (both without the heads)
+    const int n = p.sp.n_seqs, heads = p.c.n_kv_heads;
+    int* units = prefix;
+    int* slots = prefix + n + 1;
+
+    // the batch's work in (row tile) x (positions), and from it the chunk length
+    const auto tiles_of = [&](const Span& s) { return (int)(((long long)s.n * p.group + 16 * NT - 1) / (16 * NT)); };
+    long long work = 0;
+    int longest = 0;
+    for (int s = (int)threadIdx.x; s < n; s += kAttnThreads) {
+        const Span u = load_span(p.c, p.sp, s);
+        const int keys = u.n > 0 ? u.first + u.n : 0;
+        units[s] = u.n > 0 ? tiles_of(u) : 0;
+        slots[s] = keys;
+        work += (long long)units[s] * keys;
+        longest = max(longest, keys);
+    }
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) longest = max(longest, __shfl_xor(longest, d, kWave));
+    work = block_total(work, sh.sums) * heads;
+    __syncthreads();
+    if (lane_id() == 0) sh.sums[threadIdx.x / kWave] = longest;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kAttnWaves; ++w) longest = max(longest, (int)sh.sums[w]);
+    // Tiles with more positions than the chunk length L are fewer than work / L and have fewer than 2 work / L chunks in all.
+    long long len = max((work + kSlots<NT> / 2 - 1) / (kSlots<NT> / 2), (long long)((longest + kMaxChunks - 1) / kMaxChunks));
+    len = max(len, 2ll * kRound);
+    const int chunk_len = (int)min((len + kRound - 1) / kRound * kRound, 1ll << 30);
+    __syncthreads();
+
+    // prefix sums, 256 spans a round
+    int unit_base = 0, slot_base = 0;
+    for (int s0 = 0; s0 < n; s0 += kAttnThreads) {
+        const int s = s0 + (int)threadIdx.x;
+        const int tiles = s < n ? units[s] : 0, keys = s < n ? slots[s] : 0;
+        const int chunks = max((keys + chunk_len - 1) / chunk_len, 1);
+        const int mine = tiles * chunks, split = chunks > 1 ? mine : 0;
+        const long long both = (long long)mine | (long long)split << 32;
+        long long inc = both;
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) {
+            const long long o = __shfl_up(inc, d, kWave);
+            if (lane_id() >= d) inc += o;
+        }
+        if (lane_id() == kWave - 1) sh.sums[threadIdx.x / kWave] = inc;
+        __syncthreads();
+        long long before = 0, all = 0;
+#pragma unroll
+        for (int w = 0; w < kAttnWaves; ++w) {
+            if (w < (int)threadIdx.x / kWave) before += sh.sums[w];
+            all += sh.sums[w];
+        }
+        const long long at = before + inc - both;
+        if (s < n) {
+            units[s] = unit_base + (int)(at & 0xffffffff);
+            slots[s] = slot_base + (int)(at >> 32);
+        }
+        unit_base += (int)(all & 0xffffffff);
+        slot_base += (int)(all >> 32);
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) units[n] = unit_base;
+    __syncthreads();
+
+    for_each_unit(p.tickets, unit_base * heads, sh.slot, [&](int id, int) {
+        Unit u;
+        const int v = id / heads;
+        u.head = id - v * heads;
+        const int s = uniform(last_not_above(n, v, [&](int k) { return units[k]; }));
+        const Span span = load_span(p.c, p.sp, s);
+        u.slot = uniform(span.slot);
+        u.row0 = uniform(span.row0);
+        u.n = uniform(span.n);
+        u.first = uniform(span.first);
+        if (u.n <= 0) return;
+        u.chunks = max((u.first + u.n + chunk_len - 1) / chunk_len, 1);
+        const int local = v - uniform(units[s]), tiles = tiles_of(span);
+        const int back = local / u.chunks;
+        u.chunk = local - back * u.chunks;
+        u.tile = tiles - 1 - back;              // the tiles with the most positions first
+        u.slot0 = ((uniform(slots[s]) + back * u.chunks) * heads + u.head * u.chunks);
+        A::run_unit(p, u, chunk_len, sh);
+    });
+}
+
+size_t prefix_bytes(int n_seqs) { return 2 * ((size_t)n_seqs + 1) * sizeof(int); }
+
+template <int HD, int NT>
+hipError_t launch_attention(AttnParams p, int max_units, void* workspace, hipStream_t stream)
+{
+    static DeviceGrid cus;
+    const int n_cu = cus.get([] {
+        int dev = 0, n = 0;
+        if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) n = 256;
+        (void)hipFuncSetAttribute(reinterpret_cast<const void*>(attention_kernel<HD, NT>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                  (int)prefix_bytes(LQ_CACHE_MAX_SEQS));
+        return n;
+    });
+    const int grid = min(max_units, n_cu * (NT == 1 ? 3 : 2));
+    p.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + kWsHeaderBytes);
+    p.partial_bytes = (unsigned)kSlots<NT> * slot_floats<HD, NT>() * 4;
+    p.tickets = static_cast<int*>(workspace) + 4;
+    p.arrivals = static_cast<uint8_t*>(workspace) + 4 * kArrivals;
+    hipLaunchKernelGGL((attention_kernel<HD, NT>), dim3(grid), dim3(kAttnThreads), prefix_bytes(p.sp.n_seqs), stream, p);
+    return hipGetLastError();
+}
+
+// row tiles of 16: a group of query heads of one token, a draft, or a prompt
+int row_tiles(int group, int max_rows)
+{
+    const long long rows = (long long)group * max_rows;
+    return rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
 }
 
 }  // namespace
@@ -93,8 +568,11 @@ __global__ __launch_bounds__(64) void attention_kernel(AttnParams p)
 
 extern "C" size_t lora_cache_attention_workspace_bytes(const lq_cache* host_cache, int32_t n_heads, int32_t max_rows)
 {
-    if (!host_cache || n_heads <= 0 || max_rows <= 0) return 0;
-    return LQ_CACHE_MIN_WORKSPACE;
+    using namespace lq;
+    if (!host_cache || host_cache->n_kv_heads <= 0 || n_heads <= 0 || n_heads % host_cache->n_kv_heads || max_rows <= 0) return 0;
+    const int nt = row_tiles(n_heads / host_cache->n_kv_heads, max_rows);
+    const size_t slots = nt == 1 ? kSlots<1> : nt == 2 ? kSlots<2> : kSlots<4>;
+    return kWsHeaderBytes + slots * 16 * nt * ((size_t)host_cache->head_dim + 2) * 4;
 }
 
 extern "C" lq_status lora_cache_attention(const void* q, int64_t ldq, void* out, int64_t ldo, int32_t n_rows, int32_t n_heads, float scale,
@@ -107,23 +585,38 @@ extern "C" lq_status lora_cache_attention(const void* q, int64_t ldq, void* out,
     lq_status st = check_spans(host_cache, pages, row_starts, first, n_seqs, n_rows);
     if (st == LQ_OK) st = cache_view(host_cache, workspace, &p.c);
     if (st != LQ_OK) return st;
-    if (n_heads <= 0 || n_heads % host_cache->n_kv_heads || max_rows <= 0) return LQ_ERR_INVALID_ARG;
-    if (ldq < (int64_t)n_heads * host_cache->head_dim || ldo < (int64_t)n_heads * host_cache->head_dim) return LQ_ERR_INVALID_ARG;
+    const int hd = host_cache->head_dim, kv = host_cache->n_kv_heads;
+    if (n_heads <= 0 || n_heads % kv || max_rows <= 0) return LQ_ERR_INVALID_ARG;
+    if (ldq < (int64_t)n_heads * hd || ldo < (int64_t)n_heads * hd) return LQ_ERR_INVALID_ARG;
     if (n_rows > 0 && (!q || !out || q == out)) return LQ_ERR_INVALID_ARG;
     if (!(scale > -__builtin_inff() && scale < __builtin_inff())) return LQ_ERR_INVALID_ARG;
-    if (n_heads > LQ_CACHE_MAX_HEADS || n_seqs > LQ_CACHE_MAX_SEQS) return LQ_ERR_UNSUPPORTED;
+    if (n_heads > LQ_CACHE_MAX_HEADS || n_seqs > LQ_CACHE_MAX_SEQS || n_rows > LQ_CACHE_MAX_ROWS) return LQ_ERR_UNSUPPORTED;
     if ((ldq % 8) || (ldo % 8) || !aligned16(q) || !aligned16(out)) return LQ_ERR_UNSUPPORTED;
     if (!workspace || !aligned16(workspace) || workspace_bytes < lora_cache_attention_workspace_bytes(host_cache, n_heads, max_rows))
         return LQ_ERR_WORKSPACE;
     if (n_seqs == 0 || n_rows == 0) return LQ_OK;
     p.sp = Spans{slots, row_starts, first, n_seqs, n_rows};
-    p.q = static_cast<const u16*>(q); p.ldq = ldq;
-    p.out = static_cast<u16*>(out); p.ldo = ldo;
+    p.q = static_cast<const u16*>(q);
+    p.ldq = ldq;
+    p.out = static_cast<u16*>(out);
+    p.ldo = ldo;
     p.pages = static_cast<const uint8_t*>(pages);
     p.n_heads = n_heads;
-    p.group = n_heads / host_cache->n_kv_heads;
-    p.scale = scale;
-    const auto kernel = host_cache->head_dim == 128 ? attention_kernel<128> : attention_kernel<64>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)n_rows * (unsigned)n_heads), dim3(64), 0, static_cast<hipStream_t>(stream), p);
-    return hipGetLastError() == hipSuccess ? LQ_OK : LQ_ERR_HIP;
+    p.group = n_heads / kv;
+    // (not zero: a masked score is -infinity times this; 1e-30 of a score is as good as none of it)
+    p.c_log2 = __builtin_fmaxf(__builtin_fabsf(scale) * 1.44269504f, 1e-30f);
+    p.q_sign = scale < 0.f ? 0x80008000u : 0u;
+    const int nt = row_tiles(p.group, max_rows);
+    // no more workgroups than there can be units
+    const int64_t tiles = (int64_t)n_rows * p.group / (16 * nt) + n_seqs;
+    const int64_t chunks = (p.c.max_len + 2 * kRound - 1) / (2 * kRound);
+    const int64_t units = tiles * kv * (chunks < kMaxChunks ? chunks : kMaxChunks);
+    const int max_units = (int)(units < (1 << 20) ? units : 1 << 20);
+    const hipStream_t hs = static_cast<hipStream_t>(stream);
+    hipError_t e;
+    if (hd == 128) e = nt == 1 ? launch_attention<128, 1>(p, max_units, workspace, hs) : nt == 2 ? launch_attention<128, 2>(p, max_units, workspace, hs)
+                                                                                            : launch_attention<128, 4>(p, max_units, workspace, hs);
+    else e = nt == 1 ? launch_attention<64, 1>(p, max_units, workspace, hs) : nt == 2 ? launch_attention<64, 2>(p, max_units, workspace, hs)
+                                                                                       : launch_attention<64, 4>(p, max_units, workspace, hs);
+    return e == hipSuccess ? LQ_OK : LQ_ERR_HIP;
 }
