@@ -50,13 +50,15 @@ struct AttnParams {
 
 template <int HD, int NT> constexpr int slot_floats() { return 16 * NT * (HD + 2); }
 
-// codes of a step: per block of 16 keys K in the A operand layout, V in words of four positions, and the two exponent bytes
+// Codes of a step: per block of 16 keys K in the A operand layout, V in words of four positions, and the two exponent bytes.
 template <int HD>
 struct Step {
     u32x4 k[2][HD / 64], v[2][HD / 64];
     unsigned int e[2];
-    bool ok[2];                 // wave uniform: the block is there
+    bool ok[2];                 // wave uniform: the block's page can be used
 };
+template <int HD>
+struct Where { const uint8_t* k[2]; const uint8_t* e[2]; bool ok[2]; };   // wave uniform
 
 __device__ __forceinline__ unsigned int to_bf16(unsigned int w, float scale, bool high)
 {
@@ -68,6 +70,15 @@ __device__ __forceinline__ bf16x8 eight_bf16(unsigned int a, float sa, unsigned 
     return __builtin_bit_cast(bf16x8, u32x4{to_bf16(a, sa, false), to_bf16(a, sa, true), to_bf16(b, sb, false), to_bf16(b, sb, true)});
 }
 __device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+// all ones where a row that sees positions up to `limit` does not see `key` (in integers: comparisons would hold a mask
+// register pair per element)
+__device__ __forceinline__ unsigned int hidden(int limit, int key, bool ok) { return (unsigned int)(((ok ? limit : -1) - key) >> 31); }
+// bits of `a` where mask is set, of v elsewhere
+__device__ __forceinline__ float select_bits(unsigned int mask, unsigned int a, float v)
+{
+    return __uint_as_float((mask & a) | (~mask & __float_as_uint(v)));
+}
 
 // maximum (sum) over the four lanes that hold one column
 __device__ __forceinline__ float column_max(float v)
@@ -118,66 +129,98 @@ struct Attention {
     static constexpr int LD = HD / 64;          // 16-byte loads of a lane for 16 keys
     static constexpr int PITCH = HD + 4;
     struct Shared {
-        float acc[kAttnWaves][16][PITCH];
+        union {
+            float acc[kAttnWaves][16][PITCH];
+            u32x4 q[NT][HD / 32][kWave];
+        };
         float m[kAttnWaves][16 * NT], l[kAttnWaves][16 * NT];
         long long sums[kAttnWaves];
         int slot[2], last, total, chunk_len;
     };
 
-    static __device__ __forceinline__ void load_step(const AttnParams& p, PageIds& ids, const Unit& u, int key0, int last_key, Step<HD>& s)
+    // The addresses of a step's two blocks.  One that is not there gets page 0's: what is read is not used.
+    static __device__ __forceinline__ Where<HD> find_step(const AttnParams& p, PageIds& ids, const Unit& u, int key0, int last_key)
     {
         const CacheView& c = p.c;
-        const int T = 1 << c.t_log2, lane = lane_id();
+        const int T = 1 << c.t_log2;
+        Where<HD> w;
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             const int key = key0 + b * kBlock;
             const bool wanted = key <= last_key;
             const int page = wanted ? ids.get(key >> c.t_log2) : -1;
-            const bool ok = page >= 0 && page < c.n_pages;
-            if (wanted && !ok && lane == 0) atomicOr(c.err, kErrBadSegment);
-            // a block that is not there reads as zeros
-            const uint8_t* at = p.pages + (ok ? page : 0) * c.page_bytes;
-            const __amdgpu_buffer_rsrc_t page_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(at), 0, ok ? (int)c.page_bytes : 0, kRawBuffer);
+            w.ok[b] = page >= 0 && page < c.n_pages;
+            if (wanted && !w.ok[b] && lane_id() == 0) atomicOr(c.err, kErrBadSegment);
             const int in = key & (T - 1);
-            const int k_off = u.head * 2 * T * HD + in * HD, v_off = k_off + T * HD;
-            s.e[b] = __builtin_amdgcn_raw_buffer_load_b16(page_rsrc, 0, c.scale_off + (u.head * (T / kBlock) + in / kBlock) * 2, 0);
-#pragma unroll
-            for (int j = 0; j < LD; ++j)
-                s.k[b][j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(page_rsrc, (lane & 15) * HD + (lane >> 4) * 16 + 64 * j, k_off, 0));
-#pragma unroll
-            for (int j = 0; j < LD; ++j)
-                s.v[b][j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(page_rsrc, (lane >> 4) * 4 * HD + (lane & 15) * 4 * D + 16 * j, v_off, 0));
-            s.ok[b] = ok;
+            const uint8_t* at = p.pages + (w.ok[b] ? page : 0) * c.page_bytes;
+            w.k[b] = at + (u.head * 2 * T + in) * HD;
+            w.e[b] = at + c.scale_off + (u.head * (T / kBlock) + in / kBlock) * 2;
         }
+        return w;
+    }
+    static __device__ __forceinline__ void load_k(const Where<HD>& w, Step<HD>& s)
+    {
+        const unsigned int lane = lane_id(), off = (lane & 15) * HD + (lane >> 4) * 16;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            s.ok[b] = w.ok[b];
+            s.e[b] = *reinterpret_cast<const u16*>(w.e[b]);
+#pragma unroll
+            for (int j = 0; j < LD; ++j) s.k[b][j] = *reinterpret_cast<const u32x4*>(w.k[b] + off + 64 * j);
+        }
+    }
+    static __device__ __forceinline__ void load_v(const AttnParams& p, const Where<HD>& w, Step<HD>& s)
+    {
+        const unsigned int lane = lane_id(), off = (lane >> 4) * 4 * HD + (lane & 15) * 4 * D;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int j = 0; j < LD; ++j) s.v[b][j] = *reinterpret_cast<const u32x4*>(w.k[b] + ((unsigned)HD << p.c.t_log2) + off + 16 * j);
     }
 
     // One unit's chunk: the wave's share of the positions [begin, end).
     struct State { f32x4 o[NT][D]; float m[NT], l[NT]; };
 
-    static __device__ __forceinline__ void one_step(const Step<HD>& s, const bf16x8 (&q)[NT][HD / 32], const int (&limit)[NT], int key0, int last_key,
-                                                    bool masked, float c_log2, State& st)
+    struct Scores { f32x4 s[2][NT]; };
+    static constexpr bool kSharedQ = NT >= 4;   // Q's fragments in LDS (the waves have the same rows): 64 registers less
+
+    static __device__ __forceinline__ void scores(const Step<HD>& s, const bf16x8 (&q)[kSharedQ ? 1 : NT][HD / 32], const Shared& sh, Scores& sc)
     {
-        const int kg = lane_id() >> 4;
-        f32x4 sc[2][NT];
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            const float ks = block_scale(s.e[b] & 0xffu);
+        for (int b = 0; b < 2; ++b)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) sc[b][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int n = 0; n < NT; ++n) sc.s[b][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if constexpr (kSharedQ) asm volatile("" ::: "memory");   // (read again every step: kept in registers, Q would displace the sums)
+        const float k0 = block_scale(s.e[0] & 0xffu), k1 = block_scale(s.e[1] & 0xffu);
 #pragma unroll
-            for (int j = 0; j < LD; ++j)
+        for (int j = 0; j < LD; ++j)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const bf16x8 a = h == 0 ? eight_bf16(s.k[b][j].x, ks, s.k[b][j].y, ks) : eight_bf16(s.k[b][j].z, ks, s.k[b][j].w, ks);
+            for (int h = 0; h < 2; ++h) {
+                const bf16x8 a0 = h == 0 ? eight_bf16(s.k[0][j].x, k0, s.k[0][j].y, k0) : eight_bf16(s.k[0][j].z, k0, s.k[0][j].w, k0);
+                const bf16x8 a1 = h == 0 ? eight_bf16(s.k[1][j].x, k1, s.k[1][j].y, k1) : eight_bf16(s.k[1][j].z, k1, s.k[1][j].w, k1);
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) sc[b][n] = mfma(a, q[n][2 * j + h], sc[b][n]);
+                for (int n = 0; n < NT; ++n) {
+                    bf16x8 qf;
+                    if constexpr (kSharedQ) qf = __builtin_bit_cast(bf16x8, sh.q[n][2 * j + h][lane_id()]);
+                    else qf = q[n][2 * j + h];
+                    sc.s[0][n] = mfma(a0, qf, sc.s[0][n]);
+                    sc.s[1][n] = mfma(a1, qf, sc.s[1][n]);
                 }
-        }
+            }
+    }
+
+    // probabilities of a step, and its share of O^T
+    static __device__ __forceinline__ void accumulate(const u32x4 (&v)[2][LD], bool ok0, bool ok1, Scores& scores, const unsigned int (&e)[2],
+                                                      const int (&limit)[NT], int key0, int last_key, bool masked, float c_log2, State& st)
+    {
+        const bool ok[2] = {ok0, ok1};
+        const int kg = lane_id() >> 4;
+        f32x4 (&sc)[2][NT] = scores.s;
         unsigned int vw[2][D];
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
-            for (int i = 0; i < D; ++i) vw[b][i] = s.v[b][i / 4][i % 4];
+            for (int i = 0; i < D; ++i) vw[b][i] = v[b][i / 4][i % 4];
         if (masked) {
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
@@ -186,23 +229,28 @@ struct Attention {
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
-                        if (!s.ok[b] || key + r > limit[n]) sc[b][n][r] = -__builtin_inff();
+                        sc[b][n][r] = select_bits(hidden(limit[n], key + r, ok[b]), 0xff800000u, sc[b][n][r]);   // -infinity
                 // what lies in the page behind the last position that any row sees is nobody's
                 const int live = last_key + 1 - key;
-                const unsigned int keep = live >= 4 ? ~0u : live <= 0 ? 0u : (1u << (8 * live)) - 1u;
+                const unsigned int keep = !ok[b] || live <= 0 ? 0u : live >= 4 ? ~0u : (1u << (8 * live)) - 1u;
 #pragma unroll
                 for (int i = 0; i < D; ++i) vw[b][i] &= keep;
             }
         }
-        bf16x8 pt[NT];
+        float top[NT];
+        bool grows = false;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             float t = sc[0][n][0];
 #pragma unroll
             for (int r = 1; r < 8; ++r) t = fmaxf(t, sc[r / 4][n][r % 4]);
-            t = column_max(t) * c_log2;
-            if (__any(t > st.m[n] + kLazy)) {
-                const float m = fmaxf(st.m[n], t);
+            top[n] = column_max(t) * c_log2;
+            grows = grows || top[n] > st.m[n] + kLazy;
+        }
+        if (__any(grows)) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const float m = fmaxf(st.m[n], top[n]);
                 const float a = m == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(st.m[n] - m);
                 st.m[n] = m;
                 st.l[n] *= a;
@@ -211,6 +259,10 @@ struct Attention {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) st.o[n][i][r] *= a;
             }
+        }
+        bf16x8 pt[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
             const float m = st.m[n] == -__builtin_inff() ? 0.f : st.m[n];   // (nothing seen yet: 2^-inf = 0)
             float e[8], sum = 0.f;
 #pragma unroll
@@ -236,7 +288,7 @@ struct Attention {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const int key = key0 + (r / 2) * kBlock + 4 * kg + 2 * (r % 2);
-                        seen[n][r] = (s.ok[r / 2] && key <= limit[n] ? 0x3f80u : 0u) | (s.ok[r / 2] && key + 1 <= limit[n] ? 0x3f800000u : 0u);
+                        seen[n][r] = (~hidden(limit[n], key, ok[r / 2]) & 0x3f80u) | (~hidden(limit[n], key + 1, ok[r / 2]) & 0x3f800000u);
                     }
 #pragma unroll
                 for (int i = 0; i < D; ++i) {
@@ -253,12 +305,12 @@ struct Attention {
                         const f32x4 hit = mfma(a, __builtin_bit_cast(bf16x8, u32x4{seen[n][0], seen[n][1], seen[n][2], seen[n][3]}), f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
-                            if (hit[r] > 0.f) st.o[n][i][r] = __builtin_nanf("");
+                            st.o[n][i][r] = select_bits((unsigned int)(-(int)__float_as_uint(hit[r]) >> 31), 0x7fc00000u, st.o[n][i][r]);   // a count
                     }
                 }
             }
         }
-        const float v0 = block_scale(s.e[0] >> 8), v1 = block_scale(s.e[1] >> 8);
+        const float v0 = ok[0] ? block_scale(e[0] >> 8) : 1.f, v1 = ok[1] ? block_scale(e[1] >> 8) : 1.f;
 #pragma unroll
         for (int i = 0; i < D; ++i) {
             const bf16x8 a = eight_bf16(vw[0][i], v0, vw[1][i], v1);
@@ -277,7 +329,7 @@ struct Attention {
         const int begin = u.chunk * chunk_len, end = min(begin + chunk_len, last_key + 1);
         const int first_pos = u.first + row_base / p.group;                       // the first row's
 
-        bf16x8 q[NT][HD / 32];
+        bf16x8 q[kSharedQ ? 1 : NT][HD / 32];
         int limit[NT];
         State st;
 #pragma unroll
@@ -285,37 +337,66 @@ struct Attention {
             const int r = row_base + 16 * n + col;
             const int token = r / p.group, h = u.head * p.group + r % p.group;
             limit[n] = r < rows ? u.first + token : -1;
+            st.m[n] = -__builtin_inff();
+            st.l[n] = 0.f;
+#pragma unroll
+            for (int i = 0; i < D; ++i) st.o[n][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (kSharedQ && n % kAttnWaves != wave) continue;
             const u16* src = p.q + (long long)(u.row0 + token) * p.ldq + h * HD + kg * 16;
 #pragma unroll
             for (int j = 0; j < HD / 32; ++j) {
                 u32x4 w{0, 0, 0, 0};
                 if (r < rows) w = *reinterpret_cast<const u32x4*>(src + (j / 2) * 64 + (j % 2) * 8);
                 w.x ^= p.q_sign; w.y ^= p.q_sign; w.z ^= p.q_sign; w.w ^= p.q_sign;
-                q[n][j] = __builtin_bit_cast(bf16x8, w);
+                if constexpr (kSharedQ) sh.q[n][j][lane] = w;
+                else q[n][j] = __builtin_bit_cast(bf16x8, w);
             }
-            st.m[n] = -__builtin_inff();
-            st.l[n] = 0.f;
-#pragma unroll
-            for (int i = 0; i < D; ++i) st.o[n][i] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
+        if (kSharedQ) __syncthreads();
 
         int key = begin + wave * kStep;
         if (key < end) {
             PageIds ids;
             ids.start(c.table + (long long)u.slot * c.max_pages, (last_key >> c.t_log2) + 1, key >> c.t_log2);
             Step<HD> s;
-            load_step(p, ids, u, key, last_key, s);
-            while (true) {
-                const int next = key + kRound;
-                Step<HD> ahead = s;
-                if (next < end) load_step(p, ids, u, next, last_key, ahead);
-                const bool masked = key + kStep - 1 > first_pos || !s.ok[0] || !s.ok[1];
-                one_step(s, q, limit, key, last_key, masked, p.c_log2, st);
-                if (next >= end) break;
-                key = next;
-                s = ahead;
+            Where<HD> w = find_step(p, ids, u, key, last_key);
+            load_k(w, s);
+            load_v(p, w, s);
+            const auto is_masked = [&](const Step<HD>& t) { return key + kStep - 1 > first_pos || !t.ok[0] || !t.ok[1]; };
+            if constexpr (NT >= 4) {
+                // K is free for the next step's codes once the scores are there, V at the step's end (behind the last step the
+                // same codes are requested again: no branch)
+                for (; key < end; key += kRound) {
+                    const int next = key + kRound < end ? key + kRound : key;
+                    Scores sc;
+                    scores(s, q, sh, sc);
+                    const bool masked = is_masked(s), ok0 = s.ok[0], ok1 = s.ok[1];
+                    const unsigned int e[2] = {s.e[0], s.e[1]};
+                    w = find_step(p, ids, u, next, last_key);
+                    load_k(w, s);
+                    accumulate(s.v, ok0, ok1, sc, e, limit, key, last_key, masked, p.c_log2, st);
+                    load_v(p, w, s);
+                }
+            } else {
+                // memory bound: all of the next step's codes are requested a step ahead
+                while (true) {
+                    const int next = key + kRound;
+                    Step<HD> ahead = s;
+                    if (next < end) {
+                        w = find_step(p, ids, u, next, last_key);
+                        load_k(w, ahead);
+                        load_v(p, w, ahead);
+                    }
+                    Scores sc;
+                    scores(s, q, sh, sc);
+                    accumulate(s.v, s.ok[0], s.ok[1], sc, s.e, limit, key, last_key, is_masked(s), p.c_log2, st);
+                    if (next >= end) break;
+                    key = next;
+                    s = ahead;
+                }
             }
         }
+        if (kSharedQ) __syncthreads();          // acc takes q's place
 
         // the waves' maxima and sums
 #pragma unroll
@@ -476,7 +557,7 @@ __global__ __launch_bounds__(kAttnThreads, NT == 1 ? 3 : 2) void attention_kerne
     // Tiles with more positions than the chunk length L are fewer than work / L and have fewer than 2 work / L chunks in all.
     long long len = max((work + kSlots<NT> / 2 - 1) / (kSlots<NT> / 2), (long long)((longest + kMaxChunks - 1) / kMaxChunks));
     len = max(len, 2ll * kRound);
-    const int chunk_len = (int)min((len + kRound - 1) / kRound * kRound, 1ll << 30);
+    const int chunk_len = uniform((int)min((len + kRound - 1) / kRound * kRound, 1ll << 30));
     __syncthreads();
 
     // prefix sums, 256 spans a round
@@ -513,7 +594,7 @@ __global__ __launch_bounds__(kAttnThreads, NT == 1 ? 3 : 2) void attention_kerne
     if (threadIdx.x == 0) units[n] = unit_base;
     __syncthreads();
 
-    for_each_unit(p.tickets, unit_base * heads, sh.slot, [&](int id, int) {
+    for_each_unit(p.tickets, uniform(unit_base) * heads, sh.slot, [&](int id, int) {
         Unit u;
         const int v = id / heads;
         u.head = id - v * heads;
