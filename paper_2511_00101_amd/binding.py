@@ -407,6 +407,8 @@ class PagedCache:
         self.struct = _CacheStruct(n_kv_heads, head_dim, page_tokens, refs.numel(), table.shape[0], table.shape[1],
                                    table.data_ptr(), lens.data_ptr(), refs.data_ptr())
         self.ref = ctypes.addressof(self.struct)
+        self.bases = [p.data_ptr() for p in self.pages]
+        self.device_index = refs.get_device()
 
     @staticmethod
     def empty(n_layers: int, n_kv_heads: int, head_dim: int, page_tokens: int, n_pages: int, n_slots: int, max_pages: int,
@@ -433,85 +435,90 @@ def lora_cache_attention_workspace_bytes(cache: PagedCache, n_heads: int, max_ro
     return int(lib().lora_cache_attention_workspace_bytes(cache.ref, n_heads, max_rows))
 
 
-def _index(t: Optional[torch.Tensor], n: int) -> Optional[int]:
-    if t is None:
-        return None
-    assert t.dtype == torch.int32 and t.is_contiguous() and t.numel() == n
+_I32, _BF16 = torch.int32, torch.bfloat16
+
+
+def _index(t: torch.Tensor, n: int) -> int:
+    assert t.dtype is _I32 and t.numel() == n and t.is_contiguous()
     return t.data_ptr()
 
 
-def _workspace_args(workspace):
-    return _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size()
+def _cache_stream(cache: PagedCache, stream) -> Optional[int]:
+    """The stream to launch on: the current one of the cache's device, which has to be the current device.  (Read as a raw handle: a
+    decode step's calls are as short as what it costs to make a torch.cuda.Stream of it.)"""
+    if cache.device_index != torch.cuda.current_device():
+        raise ValueError(f"the cache lies on cuda:{cache.device_index}, the current device is cuda:{torch.cuda.current_device()}")
+    return torch._C._cuda_getCurrentRawStream(cache.device_index) if stream is None else _stream(stream)
+
+
+def _call_cache(name: str, *args) -> None:
+    st = getattr(lib(), name)(*args)
+    if st != LQ_OK:
+        raise LqError(st, name)
 
 
 def lora_cache_reserve(cache: PagedCache, slots: torch.Tensor, add: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
     """Pages for add[i] more positions of slot slots[i]."""
     n = slots.numel()
-    st = lib().lora_cache_reserve(cache.ref, _index(slots, n), _index(add, n), n, *_workspace_args(workspace), _stream(stream))
-    if st != LQ_OK:
-        raise LqError(st, "lora_cache_reserve")
+    _call_cache("lora_cache_reserve", cache.ref, _index(slots, n), _index(add, n), n, workspace.data_ptr(), workspace.nbytes,
+                _cache_stream(cache, stream))
 
 
 def lora_cache_fork(cache: PagedCache, src_slots: torch.Tensor, dst_slots: torch.Tensor, workspace: torch.Tensor,
                     keep: Optional[torch.Tensor] = None, stream=None) -> None:
     """Slots dst_slots become copies of (the first `keep` positions of) slots src_slots, in all layers."""
     n = src_slots.numel()
-    st = lib().lora_cache_fork(cache.ref, _index(src_slots, n), _index(dst_slots, n), _index(keep, n), n, _ptr(cache.pools), len(cache.pages),
-                               *_workspace_args(workspace), _stream(stream))
-    if st != LQ_OK:
-        raise LqError(st, "lora_cache_fork")
+    _call_cache("lora_cache_fork", cache.ref, _index(src_slots, n), _index(dst_slots, n), None if keep is None else _index(keep, n), n,
+                cache.pools.data_ptr(), len(cache.pages), workspace.data_ptr(), workspace.nbytes, _cache_stream(cache, stream))
 
 
 def lora_cache_free(cache: PagedCache, slots: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
+    """The slots become empty; pages that no other slot holds are free."""
     n = slots.numel()
-    st = lib().lora_cache_free(cache.ref, _index(slots, n), n, *_workspace_args(workspace), _stream(stream))
-    if st != LQ_OK:
-        raise LqError(st, "lora_cache_free")
+    _call_cache("lora_cache_free", cache.ref, _index(slots, n), n, workspace.data_ptr(), workspace.nbytes, _cache_stream(cache, stream))
 
 
 def lora_cache_compact(cache: PagedCache, n_live: Optional[torch.Tensor], workspace: torch.Tensor, stream=None) -> None:
     """Live pages move to the lowest numbers; n_live int32[1] (or None) receives how many there are."""
-    st = lib().lora_cache_compact(cache.ref, _ptr(cache.pools), len(cache.pages), _index(n_live, 1), *_workspace_args(workspace),
-                                  _stream(stream))
-    if st != LQ_OK:
-        raise LqError(st, "lora_cache_compact")
+    _call_cache("lora_cache_compact", cache.ref, cache.pools.data_ptr(), len(cache.pages), None if n_live is None else _index(n_live, 1),
+                workspace.data_ptr(), workspace.nbytes, _cache_stream(cache, stream))
 
 
-def _span_args(cache, layer, slots, row_starts, first):
-    n = first.numel()
-    return cache.ref, _ptr(cache.pages[layer]), _index(slots, n), _index(row_starts, n + 1), _index(first, n), n
+def _rows_matrix(t: torch.Tensor, width: int) -> int:
+    """Leading dimension of a bf16 row matrix."""
+    ld, one = t.stride()
+    assert t.dtype is _BF16 and one == 1 and t.shape[1] == width
+    return ld
 
 
 def _cache_rows_args(k, v, cache, layer, slots, row_starts, first, workspace, stream):
-    assert k.dtype == torch.bfloat16 and v.dtype == torch.bfloat16 and k.stride(1) == 1 and v.stride(1) == 1
-    assert k.shape == v.shape and k.shape[1] == cache.n_kv_heads * cache.head_dim
-    n_rows = int(k.shape[0])
-    return (_ptr(k), k.stride(0), _ptr(v), v.stride(0), n_rows, *_span_args(cache, layer, slots, row_starts, first),
-            *_workspace_args(workspace), _stream(stream))
+    width, n_rows, n = cache.n_kv_heads * cache.head_dim, k.shape[0], first.numel()
+    assert v.shape[0] == n_rows
+    return (k.data_ptr(), _rows_matrix(k, width), v.data_ptr(), _rows_matrix(v, width), n_rows, cache.ref, cache.bases[layer],
+            None if slots is None else _index(slots, n), _index(row_starts, n + 1), _index(first, n), n,
+            workspace.data_ptr(), workspace.nbytes, _cache_stream(cache, stream))
 
 
 def lora_cache_store_rows(k: torch.Tensor, v: torch.Tensor, cache: PagedCache, layer: int, slots: Optional[torch.Tensor],
                           row_starts: torch.Tensor, first: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
     """Rows row_starts[s] .. of k and v into positions first[s] .. of slot slots[s] (quantised), in one layer's pages."""
-    st = lib().lora_cache_store_rows(*_cache_rows_args(k, v, cache, layer, slots, row_starts, first, workspace, stream))
-    if st != LQ_OK:
-        raise LqError(st, "lora_cache_store_rows")
+    _call_cache("lora_cache_store_rows", *_cache_rows_args(k, v, cache, layer, slots, row_starts, first, workspace, stream))
 
 
 def lora_cache_load_rows(k: torch.Tensor, v: torch.Tensor, cache: PagedCache, layer: int, slots: Optional[torch.Tensor],
                          row_starts: torch.Tensor, first: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
     """The way back: k and v receive the cached values as bf16."""
-    st = lib().lora_cache_load_rows(*_cache_rows_args(k, v, cache, layer, slots, row_starts, first, workspace, stream))
-    if st != LQ_OK:
-        raise LqError(st, "lora_cache_load_rows")
+    _call_cache("lora_cache_load_rows", *_cache_rows_args(k, v, cache, layer, slots, row_starts, first, workspace, stream))
 
 
 def _attention_args(q, out, cache, layer, slots, row_starts, first, max_rows, workspace, scale, stream):
-    assert q.dtype == torch.bfloat16 and out.dtype == torch.bfloat16 and q.stride(1) == 1 and out.stride(1) == 1
-    assert q.shape == out.shape and q.shape[1] % cache.head_dim == 0
-    scale = cache.head_dim ** -0.5 if scale is None else float(scale)
-    return (_ptr(q), q.stride(0), _ptr(out), out.stride(0), int(q.shape[0]), int(q.shape[1]) // cache.head_dim, scale,
-            *_span_args(cache, layer, slots, row_starts, first), int(max_rows), *_workspace_args(workspace), _stream(stream))
+    n_rows, width = q.shape
+    n = first.numel()
+    assert out.shape[0] == n_rows and width % cache.head_dim == 0
+    return (q.data_ptr(), _rows_matrix(q, width), out.data_ptr(), _rows_matrix(out, width), n_rows, width // cache.head_dim,
+            cache.head_dim ** -0.5 if scale is None else scale, cache.ref, cache.bases[layer],
+            None if slots is None else _index(slots, n), _index(row_starts, n + 1), _index(first, n), n, max_rows,
+            workspace.data_ptr(), workspace.nbytes, _cache_stream(cache, stream))
 
 
 def lora_cache_attention(q: torch.Tensor, out: torch.Tensor, cache: PagedCache, layer: int, slots: Optional[torch.Tensor],
@@ -519,9 +526,7 @@ def lora_cache_attention(q: torch.Tensor, out: torch.Tensor, cache: PagedCache, 
                          scale: Optional[float] = None, stream=None) -> None:
     """Attention of the spans' rows (q, out: [rows, heads * head_dim]) over their slots' cached positions up to their own.
     max_rows: the longest span's rows, or a bound; scale: head_dim ** -0.5 unless given."""
-    st = lib().lora_cache_attention(*_attention_args(q, out, cache, layer, slots, row_starts, first, max_rows, workspace, scale, stream))
-    if st != LQ_OK:
-        raise LqError(st, "lora_cache_attention")
+    _call_cache("lora_cache_attention", *_attention_args(q, out, cache, layer, slots, row_starts, first, max_rows, workspace, scale, stream))
 
 
 def prepare_cache_attention(q, out, cache, layer, slots, row_starts, first, max_rows, workspace, scale=None, stream=None) -> PreparedCall:

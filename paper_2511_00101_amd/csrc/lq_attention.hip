@@ -23,13 +23,18 @@ namespace {
 constexpr int kAttnThreads = 256, kAttnWaves = kAttnThreads / kWave;
 constexpr int kStep = 32;                       // keys of a wave's step: two blocks
 constexpr int kRound = kStep * kAttnWaves;      // keys of a workgroup's round
-constexpr int kMaxChunks = 255;                 // arrivals are counted in a byte
-// Bytes of the workspace header that count the arrivals at split tiles: behind the barrier's words (kBarSub and its lines).
+// Bytes of the workspace header that count the arrivals at split tiles: behind the barrier's words (kBarSub and its lines).  A counter is
+// four bits where no tile has more than 15 chunks, else eight.
 constexpr int kArrivals = kBarSub + kBarFan * kBarLine;
 constexpr int kArrivalBytes = kWsHeaderBytes - 4 * kArrivals;
-// Partial-sum slots: a split tile has at least two, and its counter is its first slot's index / 2.
-template <int NT> constexpr int kSlots = NT == 1 ? 2 * kArrivalBytes : NT == 2 ? 2048 : 1024;
-static_assert(kSlots<1> / 2 <= kArrivalBytes && kSlots<2> / 2 <= kArrivalBytes && kSlots<4> / 2 <= kArrivalBytes, "a byte per split tile");
+// Partial-sum slots of a call: a split tile has at least two, and its counter's number is its first slot's / 2.
+template <int NT> constexpr int kSlots = NT <= 2 ? 4 * kArrivalBytes : 2 * kArrivalBytes;
+constexpr int kManyChunksSlots = 2 * kArrivalBytes;    // with counters of eight bits
+template <int HD, int NT> constexpr int kResident = HD == 64 ? (NT == 1 ? 4 : NT == 2 ? 3 : 2) : NT == 1 ? 3 : 2;   // workgroups of a CU
+constexpr int kLeastChunk = 2 * kRound;
+constexpr int kClasses = 5;
+constexpr int kKeptSpans = 1024;                // spans that a workgroup keeps in LDS (16 KB); of more, a unit's is read again
+__host__ __device__ constexpr int span_at(int n) { return (3 * n + 1 + 3) / 4 * 4; }
 constexpr float kLazy = 8.f;                    // log2 of how far a score may exceed the maximum that its exponentials use
 constexpr int kRawBuffer = 0x00020000, kSc1 = 16;   // descriptor word 3 (raw 32-bit data); device-scope cache policy
 
@@ -40,6 +45,7 @@ struct AttnParams {
     u16* out; long long ldo;
     const uint8_t* pages;
     int n_heads, group;
+    unsigned int group_magic;   // ceil(2^20 / group): x / group = x * magic >> 20 for x below 2^20 / group
     float c_log2;               // |scale| * log2(e)
     unsigned int q_sign;        // 0x80008000 where the scale is negative
     float* partial;
@@ -121,21 +127,27 @@ struct PageIds {
     }
 };
 
-struct Unit { int slot, row0, n, first, tile, head, chunk, chunks, slot0; };   // slot0: first partial-sum slot of the tile
+struct Unit { int slot, row0, n, first, tile, head, chunk, chunks, slot0, bits; };   // slot0: first partial-sum slot of the tile; bits: of a counter
 
 template <int HD, int NT>
 struct Attention {
     static constexpr int D = HD / 16;           // O^T rows of a lane's accumulator register set; also V words of a lane and block
     static constexpr int LD = HD / 64;          // 16-byte loads of a lane for 16 keys
     static constexpr int PITCH = HD + 4;
+    // Few rows: the codes are read once and bound the kernel.  Every load takes whole 128-byte lines, past the caches.
+    static constexpr bool kStream = NT < 4;
+    // head_dim 128: a load of K takes eight whole rows (lanes m < 8 of 16 the lower halves, the others the upper ones)
+    static constexpr bool kWholeRows = kStream && LD == 2;
     struct Shared {
         union {
             float acc[kAttnWaves][16][PITCH];
             u32x4 q[NT][HD / 32][kWave];
+            f32x2 ml[256 * 16];                 // of a split tile's chunks: maxima (then factors) and sums
         };
         float m[kAttnWaves][16 * NT], l[kAttnWaves][16 * NT];
         long long sums[kAttnWaves];
-        int slot[2], last, total, chunk_len;
+        int longest[kAttnWaves], scan[kAttnWaves][2], classes[kAttnWaves][kClasses];
+        int slot[2], last;
     };
 
     // The addresses of a step's two blocks.  One that is not there gets page 0's: what is read is not used.
@@ -160,22 +172,38 @@ struct Attention {
     }
     static __device__ __forceinline__ void load_k(const Where<HD>& w, Step<HD>& s)
     {
-        const unsigned int lane = lane_id(), off = (lane & 15) * HD + (lane >> 4) * 16;
+        const unsigned int lane = lane_id();
+        const unsigned int off = kWholeRows ? (lane & 7) * HD + (lane >> 3 & 1) * 64 + (lane >> 4) * 16 : (lane & 15) * HD + (lane >> 4) * 16;
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             s.ok[b] = w.ok[b];
             s.e[b] = *reinterpret_cast<const u16*>(w.e[b]);
 #pragma unroll
-            for (int j = 0; j < LD; ++j) s.k[b][j] = *reinterpret_cast<const u32x4*>(w.k[b] + off + 64 * j);
+            for (int j = 0; j < LD; ++j) s.k[b][j] = load_once<kStream>(w.k[b] + off + (kWholeRows ? 8 * HD : 64) * j);
+        }
+    }
+    // K of a block in the A operand layout: lane (m, kg), key m, word group j its codes 64 j + 16 kg .. + 15.  Lanes m and m + 8 swap what
+    // they loaded for each other where a load took eight whole rows.
+    static __device__ __forceinline__ void operand_k(const u32x4 (&loaded)[LD], u32x4 (&k)[LD])
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (kWholeRows) {
+                k[0][i] = __builtin_amdgcn_update_dpp((int)loaded[0][i], (int)loaded[1][i], 0x128, 0xf, 0xc, false);   // row_ror:8
+                k[1][i] = __builtin_amdgcn_update_dpp((int)loaded[1][i], (int)loaded[0][i], 0x128, 0xf, 0x3, false);
+            } else {
+#pragma unroll
+                for (int j = 0; j < LD; ++j) k[j][i] = loaded[j][i];
+            }
         }
     }
     static __device__ __forceinline__ void load_v(const AttnParams& p, const Where<HD>& w, Step<HD>& s)
     {
-        const unsigned int lane = lane_id(), off = (lane >> 4) * 4 * HD + (lane & 15) * 4 * D;
+        const unsigned int lane = lane_id(), off = (lane >> 4) * 4 * HD + (lane & 15) * 16;
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
-            for (int j = 0; j < LD; ++j) s.v[b][j] = *reinterpret_cast<const u32x4*>(w.k[b] + ((unsigned)HD << p.c.t_log2) + off + 16 * j);
+            for (int j = 0; j < LD; ++j) s.v[b][j] = load_once<kStream>(w.k[b] + ((unsigned)HD << p.c.t_log2) + off + 256 * j);
     }
 
     // One unit's chunk: the wave's share of the positions [begin, end).
@@ -192,12 +220,15 @@ struct Attention {
             for (int n = 0; n < NT; ++n) sc.s[b][n] = f32x4{0.f, 0.f, 0.f, 0.f};
         if constexpr (kSharedQ) asm volatile("" ::: "memory");   // (read again every step: kept in registers, Q would displace the sums)
         const float k0 = block_scale(s.e[0] & 0xffu), k1 = block_scale(s.e[1] & 0xffu);
+        u32x4 k[2][LD];
+        operand_k(s.k[0], k[0]);
+        operand_k(s.k[1], k[1]);
 #pragma unroll
         for (int j = 0; j < LD; ++j)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const bf16x8 a0 = h == 0 ? eight_bf16(s.k[0][j].x, k0, s.k[0][j].y, k0) : eight_bf16(s.k[0][j].z, k0, s.k[0][j].w, k0);
-                const bf16x8 a1 = h == 0 ? eight_bf16(s.k[1][j].x, k1, s.k[1][j].y, k1) : eight_bf16(s.k[1][j].z, k1, s.k[1][j].w, k1);
+                const bf16x8 a0 = h == 0 ? eight_bf16(k[0][j].x, k0, k[0][j].y, k0) : eight_bf16(k[0][j].z, k0, k[0][j].w, k0);
+                const bf16x8 a1 = h == 0 ? eight_bf16(k[1][j].x, k1, k[1][j].y, k1) : eight_bf16(k[1][j].z, k1, k[1][j].w, k1);
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     bf16x8 qf;
@@ -327,7 +358,14 @@ struct Attention {
         const int last_row = min(row_base + 16 * NT, rows) - 1;
         const int last_key = u.first + last_row / p.group;                        // the last position that a row of the tile sees
         const int begin = u.chunk * chunk_len, end = min(begin + chunk_len, last_key + 1);
-        const int first_pos = u.first + row_base / p.group;                       // the first row's
+        const int token0 = row_base / p.group, within0 = row_base - token0 * p.group;
+        const int first_pos = u.first + token0;                                   // the first row's
+        // token and query head of row row_base + x of the tile
+        const auto row_of = [&](int x, int& token, int& h) {
+            const int y = within0 + x, t = (int)(((unsigned)y * p.group_magic) >> 20);
+            token = token0 + t;
+            h = u.head * p.group + y - t * p.group;
+        };
 
         bf16x8 q[kSharedQ ? 1 : NT][HD / 32];
         int limit[NT];
@@ -335,7 +373,8 @@ struct Attention {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const int r = row_base + 16 * n + col;
-            const int token = r / p.group, h = u.head * p.group + r % p.group;
+            int token, h;
+            row_of(16 * n + col, token, h);
             limit[n] = r < rows ? u.first + token : -1;
             st.m[n] = -__builtin_inff();
             st.l[n] = 0.f;
@@ -423,7 +462,7 @@ struct Attention {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const f32x4 v{st.o[n][4 * i4][r] * a, st.o[n][4 * i4 + 1][r] * a, st.o[n][4 * i4 + 2][r] * a, st.o[n][4 * i4 + 3][r] * a};
-                    *reinterpret_cast<f32x4*>(&sh.acc[wave][col][(4 * kg + r) * D + 4 * i4]) = v;
+                    *reinterpret_cast<f32x4*>(&sh.acc[wave][col][64 * i4 + 16 * kg + 4 * r]) = v;
                 }
             __syncthreads();
             const int r = row_base + 16 * n + out_row;
@@ -443,7 +482,11 @@ struct Attention {
 #pragma unroll
                     for (int w = 0; w < kAttnWaves; ++w) o[i] += sh.acc[w][out_row][out_col + i];
                 }
-                if (!split) write_out(p, u, r, out_col, o, l);
+                if (!split) {
+                    int token, h;
+                    row_of(16 * n + out_row, token, h);
+                    write_out(p, u.row0 + token, h, out_col, o, l);
+                }
                 else {
                     const int at = (u.slot0 + u.chunk) * slot_bytes;
                     const int row = 16 * n + out_row;
@@ -462,10 +505,10 @@ struct Attention {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         if (threadIdx.x == 0) {
-            const int i = u.slot0 / 2, shift = 8 * (i % 4);
-            int* word = reinterpret_cast<int*>(p.arrivals) + i / 4;
+            const int i = u.slot0 / 2 * u.bits, shift = i % 32;
+            int* word = reinterpret_cast<int*>(p.arrivals) + i / 32;
             const int old = __hip_atomic_fetch_add(word, 1 << shift, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            const bool last = ((old >> shift) & 255) == u.chunks - 1;
+            const bool last = ((old >> shift) & ((1 << u.bits) - 1)) == u.chunks - 1;
             if (last) __hip_atomic_fetch_sub(word, (int)((unsigned)u.chunks << shift), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             sh.last = last;
         }
@@ -473,66 +516,90 @@ struct Attention {
         if (!sh.last) return;
         asm volatile("" ::: "memory");
         for (int n = 0; n < NT; ++n) {
-            const int row = 16 * n + out_row, r = row_base + row;
-            if (r >= rows) continue;
-            float top = -__builtin_inff();
-            for (int k = 0; k < u.chunks; ++k)
-                top = fmaxf(top, __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(part, stat_at + row * 8, (u.slot0 + k) * slot_bytes, kSc1)));
-            float o[D], l = 0.f;
+            const int live = min(rows - row_base - 16 * n, 16);                   // rows of this tile of 16, and the power of two above
+            if (live <= 0) break;
+            const int row_log2 = live <= 1 ? 0 : 32 - __builtin_clz(live - 1), mask = (1 << row_log2) - 1;
+            const auto row_bytes = [&](int row) { return (16 * n + row) * HD * 4; };
+            __syncthreads();
+            for (int i = (int)threadIdx.x; i < u.chunks << row_log2; i += kAttnThreads)
+                if ((i & mask) < live)
+                    sh.ml[i] = __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(part, stat_at + (16 * n + (i & mask)) * 8, (u.slot0 + (i >> row_log2)) * slot_bytes, kSc1));
+            __syncthreads();
+            // sixteen threads a row: its maximum, its sum, and every chunk's factor
+            const int row = (int)threadIdx.x / 16, j = (int)threadIdx.x % 16;
+            if (row < live) {
+                float top = -__builtin_inff(), l = 0.f;
+                for (int k = j; k < u.chunks; k += 16) top = fmaxf(top, sh.ml[(k << row_log2) + row].x);
+#pragma unroll
+                for (int d = 1; d < 16; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, kWave));
+                for (int k = j; k < u.chunks; k += 16) {
+                    f32x2& ml = sh.ml[(k << row_log2) + row];
+                    const float a = ml.x == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
+                    l += ml.y * a;
+                    ml.x = a;
+                }
+#pragma unroll
+                for (int d = 1; d < 16; d <<= 1) l += __shfl_xor(l, d, kWave);
+                if (j == 0) sh.l[0][row] = l;
+            }
+            __syncthreads();
+            // the chunks dealt to as many groups of threads as the rows leave; then the groups' sums in order
+            const int r = row & mask, group = row >> row_log2, groups = 16 >> row_log2;
+            float o[D];
 #pragma unroll
             for (int i = 0; i < D; ++i) o[i] = 0.f;
-#pragma unroll 4
-            for (int k = 0; k < u.chunks; ++k) {
-                const int at = (u.slot0 + k) * slot_bytes;
-                const f32x2 ml = __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(part, stat_at + row * 8, at, kSc1));
-                const float a = ml.x == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
-                l += ml.y * a;
+            if (r < live) {
+#pragma unroll 2
+                for (int k = group; k < u.chunks; k += groups) {
+                    const int at = (u.slot0 + k) * slot_bytes;
+                    const float a = sh.ml[(k << row_log2) + r].x;
 #pragma unroll
-                for (int i = 0; i < D; i += 4) {
-                    const f32x4 v = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(part, (row * HD + out_col + i) * 4, at, kSc1));
+                    for (int i = 0; i < D; i += 4) {
+                        const f32x4 v = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(part, row_bytes(r) + (out_col + i) * 4, at, kSc1));
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) o[i + x] += v[x] * a;
+                        for (int x = 0; x < 4; ++x) o[i + x] += v[x] * a;
+                    }
                 }
             }
-            write_out(p, u, r, out_col, o, l);
+            __syncthreads();
+            float* sums = &sh.acc[0][0][0];
+#pragma unroll
+            for (int i = 0; i < D; i += 4) *reinterpret_cast<f32x4*>(sums + (int)threadIdx.x * D + i) = f32x4{o[i], o[i + 1], o[i + 2], o[i + 3]};
+            __syncthreads();
+            if (group == 0 && r < live) {
+                for (int g = 1; g < groups; ++g)
+#pragma unroll
+                    for (int i = 0; i < D; ++i) o[i] += sums[((((g << row_log2) + r) * 16) + j) * D + i];
+                int token, h;
+                row_of(16 * n + r, token, h);
+                write_out(p, u.row0 + token, h, out_col, o, sh.l[0][r]);
+            }
         }
     }
 
-    static __device__ __forceinline__ void write_out(const AttnParams& p, const Unit& u, int r, int col, const float* o, float l)
+    static __device__ __forceinline__ void write_out(const AttnParams& p, int row, int h, int col, const float* o, float l)
     {
-        const int token = r / p.group, h = u.head * p.group + r % p.group;
         const float inv = l == 0.f ? 0.f : 1.f / l;
         unsigned int w[D / 2];
 #pragma unroll
         for (int i = 0; i < D / 2; ++i) w[i] = pack_bf16x2(o[2 * i] * inv, o[2 * i + 1] * inv);
-        u16* dst = p.out + (long long)(u.row0 + token) * p.ldo + h * HD + col;
+        u16* dst = p.out + (long long)row * p.ldo + h * HD + col;
         if constexpr (D == 8) *reinterpret_cast<u32x4*>(dst) = u32x4{w[0], w[1], w[2], w[3]};
         else *reinterpret_cast<u32x2*>(dst) = u32x2{w[0], w[1]};
     }
 };
 
-__device__ __forceinline__ long long block_total(long long v, long long* sums)
-{
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) v += __shfl_xor(v, d, kWave);
-    __syncthreads();
-    if (lane_id() == 0) sums[threadIdx.x / kWave] = v;
-    __syncthreads();
-    long long t = 0;
-#pragma unroll
-    for (int w = 0; w < kAttnWaves; ++w) t += sums[w];
-    return t;
-}
-
 template <int HD, int NT>
-__global__ __launch_bounds__(kAttnThreads, NT == 1 ? 3 : 2) void attention_kernel(AttnParams p)
+__global__ __launch_bounds__(kAttnThreads, (kResident<HD, NT>)) void attention_kernel(AttnParams p)
 {
     using A = Attention<HD, NT>;
     __shared__ typename A::Shared sh;
-    extern __shared__ int prefix[];             // per span: units before it; and partial-sum slots before it (both without the heads)
+    extern __shared__ int prefix[];             // in the order of work: units before a span, partial-sum slots before it (both without the heads), its number
     const int n = p.sp.n_seqs, heads = p.c.n_kv_heads;
     int* units = prefix;
-    int* slots = prefix + n + 1;
+    int* slots = units + n + 1;
+    int* order = slots + n;
+    Span* spans = reinterpret_cast<Span*>(prefix + span_at(n));      // the spans, where they are few enough to be kept
 
     // the batch's work in (row tile) x (positions), and from it the chunk length
     const auto tiles_of = [&](const Span& s) { return (int)(((long long)s.n * p.group + 16 * NT - 1) / (16 * NT)); };
@@ -541,55 +608,88 @@ __global__ __launch_bounds__(kAttnThreads, NT == 1 ? 3 : 2) void attention_kerne
     for (int s = (int)threadIdx.x; s < n; s += kAttnThreads) {
         const Span u = load_span(p.c, p.sp, s);
         const int keys = u.n > 0 ? u.first + u.n : 0;
-        units[s] = u.n > 0 ? tiles_of(u) : 0;
+        const int tiles = u.n > 0 ? tiles_of(u) : 0;
+        units[s] = tiles;
         slots[s] = keys;
-        work += (long long)units[s] * keys;
+        if (n <= kKeptSpans) spans[s] = u;
+        work += (long long)tiles * keys;
         longest = max(longest, keys);
     }
 #pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) longest = max(longest, __shfl_xor(longest, d, kWave));
-    work = block_total(work, sh.sums) * heads;
+    for (int d = 1; d < kWave; d <<= 1) {
+        longest = max(longest, __shfl_xor(longest, d, kWave));
+        work += __shfl_xor(work, d, kWave);
+    }
+    if (lane_id() == 0) {
+        sh.sums[threadIdx.x / kWave] = work;
+        sh.longest[threadIdx.x / kWave] = longest;
+    }
     __syncthreads();
-    if (lane_id() == 0) sh.sums[threadIdx.x / kWave] = longest;
-    __syncthreads();
+    work = 0;
 #pragma unroll
-    for (int w = 0; w < kAttnWaves; ++w) longest = max(longest, (int)sh.sums[w]);
-    // Tiles with more positions than the chunk length L are fewer than work / L and have fewer than 2 work / L chunks in all.
-    long long len = max((work + kSlots<NT> / 2 - 1) / (kSlots<NT> / 2), (long long)((longest + kMaxChunks - 1) / kMaxChunks));
-    len = max(len, 2ll * kRound);
+    for (int w = 0; w < kAttnWaves; ++w) {
+        work += sh.sums[w];
+        longest = max(longest, sh.longest[w]);
+    }
+    work *= heads;
+    // Tiles with more positions than the chunk length are fewer than work / length and have fewer than 2 work / length chunks in all.
+    const auto length = [&](int n_slots, int most) { return max((work + n_slots / 2 - 1) / (n_slots / 2), (long long)((longest + most - 1) / most)); };
+    const long long few = length(kSlots<NT>, 15), many = length(kManyChunksSlots, 255);
+    const int bits = uniform(few <= many ? 4 : 8);
+    const long long round = work * 2 / (int)gridDim.x + 1;            // half a unit per workgroup
+    const long long len = max(max(min(few, many), round), (long long)kLeastChunk);
     const int chunk_len = uniform((int)min((len + kRound - 1) / kRound * kRound, 1ll << 30));
-    __syncthreads();
 
-    // prefix sums, 256 spans a round
+    // Prefix sums, 256 spans a round; within a round the longest spans first (by powers of two below the longest of all), so that the
+    // tickets end evenly.
     int unit_base = 0, slot_base = 0;
     for (int s0 = 0; s0 < n; s0 += kAttnThreads) {
-        const int s = s0 + (int)threadIdx.x;
-        const int tiles = s < n ? units[s] : 0, keys = s < n ? slots[s] : 0;
+        const int s = s0 + (int)threadIdx.x, wave = (int)threadIdx.x / kWave;
+        int tiles = s < n ? units[s] : 0, keys = s < n ? slots[s] : 0;
+        const int shorter = s < n ? min(__builtin_clz(max(keys, 1)) - __builtin_clz(max(longest, 1)), kClasses - 1) : kClasses;
+        int same = 0, rank = 0;
+#pragma unroll
+        for (int k = 0; k < kClasses; ++k) {
+            const unsigned long long in = __ballot(shorter == k);
+            if (shorter == k) same = __popcll(in & ((1ull << lane_id()) - 1));
+            if (lane_id() == 0) sh.classes[wave][k] = __popcll(in);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kClasses; ++k)
+#pragma unroll
+            for (int w = 0; w < kAttnWaves; ++w)
+                if (k < shorter || (k == shorter && w < wave)) rank += sh.classes[w][k];
+        if (s < n) {
+            order[s0 + rank + same] = s;
+            units[s0 + rank + same] = tiles;
+            slots[s0 + rank + same] = keys;
+        }
+        __syncthreads();
+        tiles = s < n ? units[s] : 0;
+        keys = s < n ? slots[s] : 0;
         const int chunks = max((keys + chunk_len - 1) / chunk_len, 1);
         const int mine = tiles * chunks, split = chunks > 1 ? mine : 0;
-        const long long both = (long long)mine | (long long)split << 32;
-        long long inc = both;
-#pragma unroll
-        for (int d = 1; d < kWave; d <<= 1) {
-            const long long o = __shfl_up(inc, d, kWave);
-            if (lane_id() >= d) inc += o;
+        const int units_upto = wave_inclusive_scan(mine), slots_upto = wave_inclusive_scan(split);
+        if (lane_id() == kWave - 1) {
+            sh.scan[wave][0] = units_upto;
+            sh.scan[wave][1] = slots_upto;
         }
-        if (lane_id() == kWave - 1) sh.sums[threadIdx.x / kWave] = inc;
         __syncthreads();
-        long long before = 0, all = 0;
+        int units_at = unit_base + units_upto - mine, slots_at = slot_base + slots_upto - split;
 #pragma unroll
         for (int w = 0; w < kAttnWaves; ++w) {
-            if (w < (int)threadIdx.x / kWave) before += sh.sums[w];
-            all += sh.sums[w];
+            if (w < wave) {
+                units_at += sh.scan[w][0];
+                slots_at += sh.scan[w][1];
+            }
+            unit_base += sh.scan[w][0];
+            slot_base += sh.scan[w][1];
         }
-        const long long at = before + inc - both;
         if (s < n) {
-            units[s] = unit_base + (int)(at & 0xffffffff);
-            slots[s] = slot_base + (int)(at >> 32);
+            units[s] = units_at;
+            slots[s] = slots_at;
         }
-        unit_base += (int)(all & 0xffffffff);
-        slot_base += (int)(all >> 32);
-        __syncthreads();
     }
     if (threadIdx.x == 0) units[n] = unit_base;
     __syncthreads();
@@ -598,24 +698,25 @@ __global__ __launch_bounds__(kAttnThreads, NT == 1 ? 3 : 2) void attention_kerne
         Unit u;
         const int v = id / heads;
         u.head = id - v * heads;
-        const int s = uniform(last_not_above(n, v, [&](int k) { return units[k]; }));
-        const Span span = load_span(p.c, p.sp, s);
+        const int at = uniform(last_not_above(n, v, [&](int k) { return units[k]; })), s = uniform(order[at]);
+        const Span span = n <= kKeptSpans ? spans[s] : load_span(p.c, p.sp, s);
         u.slot = uniform(span.slot);
         u.row0 = uniform(span.row0);
         u.n = uniform(span.n);
         u.first = uniform(span.first);
         if (u.n <= 0) return;
         u.chunks = max((u.first + u.n + chunk_len - 1) / chunk_len, 1);
-        const int local = v - uniform(units[s]), tiles = tiles_of(span);
+        u.bits = bits;
+        const int local = v - uniform(units[at]);
         const int back = local / u.chunks;
         u.chunk = local - back * u.chunks;
-        u.tile = tiles - 1 - back;              // the tiles with the most positions first
-        u.slot0 = ((uniform(slots[s]) + back * u.chunks) * heads + u.head * u.chunks);
+        u.tile = tiles_of(Span{u.slot, u.row0, u.n, u.first}) - 1 - back;      // the tiles with the most positions first
+        u.slot0 = ((uniform(slots[at]) + back * u.chunks) * heads + u.head * u.chunks);
         A::run_unit(p, u, chunk_len, sh);
     });
 }
 
-size_t prefix_bytes(int n_seqs) { return 2 * ((size_t)n_seqs + 1) * sizeof(int); }
+size_t prefix_bytes(int n_seqs) { return (size_t)span_at(n_seqs) * sizeof(int) + (n_seqs <= kKeptSpans ? (size_t)n_seqs * sizeof(Span) : 0); }
 
 template <int HD, int NT>
 hipError_t launch_attention(AttnParams p, int max_units, void* workspace, hipStream_t stream)
@@ -625,10 +726,10 @@ hipError_t launch_attention(AttnParams p, int max_units, void* workspace, hipStr
         int dev = 0, n = 0;
         if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) n = 256;
         (void)hipFuncSetAttribute(reinterpret_cast<const void*>(attention_kernel<HD, NT>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                  (int)prefix_bytes(LQ_CACHE_MAX_SEQS));
+                                  (int)(prefix_bytes(LQ_CACHE_MAX_SEQS) > prefix_bytes(kKeptSpans) ? prefix_bytes(LQ_CACHE_MAX_SEQS) : prefix_bytes(kKeptSpans)));
         return n;
     });
-    const int grid = min(max_units, n_cu * (NT == 1 ? 3 : 2));
+    const int grid = min(max_units, n_cu * kResident<HD, NT>);
     p.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + kWsHeaderBytes);
     p.partial_bytes = (unsigned)kSlots<NT> * slot_floats<HD, NT>() * 4;
     p.tickets = static_cast<int*>(workspace) + 4;
@@ -652,7 +753,7 @@ extern "C" size_t lora_cache_attention_workspace_bytes(const lq_cache* host_cach
     using namespace lq;
     if (!host_cache || host_cache->n_kv_heads <= 0 || n_heads <= 0 || n_heads % host_cache->n_kv_heads || max_rows <= 0) return 0;
     const int nt = row_tiles(n_heads / host_cache->n_kv_heads, max_rows);
-    const size_t slots = nt == 1 ? kSlots<1> : nt == 2 ? kSlots<2> : kSlots<4>;
+    const size_t slots = nt <= 2 ? kSlots<2> : kSlots<4>;
     return kWsHeaderBytes + slots * 16 * nt * ((size_t)host_cache->head_dim + 2) * 4;
 }
 
@@ -686,12 +787,13 @@ extern "C" lq_status lora_cache_attention(const void* q, int64_t ldq, void* out,
     p.group = n_heads / kv;
     // (not zero: a masked score is -infinity times this; 1e-30 of a score is as good as none of it)
     p.c_log2 = __builtin_fmaxf(__builtin_fabsf(scale) * 1.44269504f, 1e-30f);
+    p.group_magic = (unsigned)(((1 << 20) + p.group - 1) / p.group);
     p.q_sign = scale < 0.f ? 0x80008000u : 0u;
     const int nt = row_tiles(p.group, max_rows);
     // no more workgroups than there can be units
     const int64_t tiles = (int64_t)n_rows * p.group / (16 * nt) + n_seqs;
-    const int64_t chunks = (p.c.max_len + 2 * kRound - 1) / (2 * kRound);
-    const int64_t units = tiles * kv * (chunks < kMaxChunks ? chunks : kMaxChunks);
+    const int64_t chunks = (p.c.max_len + kLeastChunk - 1) / kLeastChunk;
+    const int64_t units = tiles * kv * (chunks < 255 ? chunks : 255);
     const int max_units = (int)(units < (1 << 20) ? units : 1 << 20);
     const hipStream_t hs = static_cast<hipStream_t>(stream);
     hipError_t e;
