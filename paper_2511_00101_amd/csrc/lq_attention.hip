@@ -156,18 +156,22 @@ struct Attention {
         const CacheView& c = p.c;
         const int T = 1 << c.t_log2;
         Where<HD> w;
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            const int key = key0 + b * kBlock;
-            const bool wanted = key <= last_key;
-            const int page = wanted ? ids.get(key >> c.t_log2) : -1;
+        const auto block = [&](int b, int page, bool wanted) {
+            const int in = (key0 + b * kBlock) & (T - 1);
             w.ok[b] = page >= 0 && page < c.n_pages;
             if (wanted && !w.ok[b] && lane_id() == 0) atomicOr(c.err, kErrBadSegment);
-            const int in = key & (T - 1);
             const uint8_t* at = p.pages + (w.ok[b] ? page : 0) * c.page_bytes;
             w.k[b] = at + (u.head * 2 * T + in) * HD;
             w.e[b] = at + c.scale_off + (u.head * (T / kBlock) + in / kBlock) * 2;
-        }
+        };
+        const int first = ids.get(key0 >> c.t_log2);
+        block(0, first, true);
+        const bool wanted = key0 + kBlock <= last_key;
+        if (c.t_log2 > 4) {             // (a step's blocks share a page)
+            w.ok[1] = w.ok[0] && wanted;
+            w.k[1] = w.k[0] + kBlock * HD;
+            w.e[1] = w.e[0] + 2;
+        } else block(1, wanted ? ids.get((key0 + kBlock) >> c.t_log2) : -1, wanted);
         return w;
     }
     static __device__ __forceinline__ void load_k(const Where<HD>& w, Step<HD>& s)
@@ -268,20 +272,21 @@ struct Attention {
                 for (int i = 0; i < D; ++i) vw[b][i] &= keep;
             }
         }
+        // Only a score that exceeds its row's maximum by more than kLazy changes the maximum: every lane looks at its own, and the
+        // columns' maxima are worked out when one does.
         float top[NT];
         bool grows = false;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            float t = sc[0][n][0];
+            top[n] = sc[0][n][0];
 #pragma unroll
-            for (int r = 1; r < 8; ++r) t = fmaxf(t, sc[r / 4][n][r % 4]);
-            top[n] = column_max(t) * c_log2;
-            grows = grows || top[n] > st.m[n] + kLazy;
+            for (int r = 1; r < 8; ++r) top[n] = fmaxf(top[n], sc[r / 4][n][r % 4]);
+            grows = grows || __builtin_fmaf(top[n], c_log2, -kLazy) > st.m[n];
         }
         if (__any(grows)) {
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                const float m = fmaxf(st.m[n], top[n]);
+                const float m = fmaxf(st.m[n], column_max(top[n]) * c_log2);
                 const float a = m == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(st.m[n] - m);
                 st.m[n] = m;
                 st.l[n] *= a;
