@@ -116,15 +116,16 @@ struct PageIds {
         now = load(batch);
         next = load(batch + 1);
     }
-    __device__ __forceinline__ int get(int entry)
+    // makes `entry` (wave uniform) one of the lanes'; entries are asked for in order
+    __device__ __forceinline__ void reach(int entry)
     {
-        if (entry / kWave != batch) {   // wave uniform; entries are asked for in order
+        if (entry / kWave != batch) {
             now = next;
             batch = entry / kWave;
             next = load(batch + 1);
         }
-        return lane_value(now, entry % kWave);
     }
+    __device__ __forceinline__ int get(int entry) const { return lane_value(now, entry % kWave); }
 };
 
 struct Unit { int slot, row0, n, first, tile, head, chunk, chunks, slot0, bits; };   // slot0: first partial-sum slot of the tile; bits: of a counter
@@ -141,7 +142,10 @@ struct Attention {
     struct Shared {
         union {
             float acc[kAttnWaves][16][PITCH];
-            u32x4 q[NT][HD / 32][kWave];
+            struct {
+                u32x4 q[NT][HD / 32][kWave];    // fragments: of bf16 values; or of codes, high parts and low parts
+                unsigned int q_exp[NT][16];
+            };
             f32x2 ml[256 * 16];                 // of a split tile's chunks: maxima (then factors) and sums
         };
         float m[kAttnWaves][16 * NT], l[kAttnWaves][16 * NT];
@@ -150,28 +154,26 @@ struct Attention {
         int slot[2], last;
     };
 
-    // The addresses of a step's two blocks.  One that is not there gets page 0's: what is read is not used.
-    static __device__ __forceinline__ Where<HD> find_step(const AttnParams& p, PageIds& ids, const Unit& u, int key0, int last_key)
+    // The addresses of a step's two blocks (their entries lie in one batch: a step begins at a multiple of 32 positions).  A block that is
+    // not there gets page 0's: what is read is not used.  bad: whether a position that a row sees has no usable page.
+    static __device__ __forceinline__ Where<HD> find_step(const AttnParams& p, PageIds& ids, const Unit& u, int key0, int last_key, bool& bad)
     {
         const CacheView& c = p.c;
         const int T = 1 << c.t_log2;
         Where<HD> w;
-        const auto block = [&](int b, int page, bool wanted) {
-            const int in = (key0 + b * kBlock) & (T - 1);
-            w.ok[b] = page >= 0 && page < c.n_pages;
-            if (wanted && !w.ok[b] && lane_id() == 0) atomicOr(c.err, kErrBadSegment);
-            const uint8_t* at = p.pages + (w.ok[b] ? page : 0) * c.page_bytes;
+        ids.reach(key0 >> c.t_log2);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const int key = key0 + b * kBlock, in = key & (T - 1);
+            const bool wanted = key <= last_key;
+            const int page = ids.get(min(key, last_key) >> c.t_log2);
+            const bool usable = page >= 0 && page < c.n_pages;
+            bad = bad || !usable;
+            w.ok[b] = usable && wanted;
+            const uint8_t* at = p.pages + (usable ? page : 0) * c.page_bytes;
             w.k[b] = at + (u.head * 2 * T + in) * HD;
             w.e[b] = at + c.scale_off + (u.head * (T / kBlock) + in / kBlock) * 2;
-        };
-        const int first = ids.get(key0 >> c.t_log2);
-        block(0, first, true);
-        const bool wanted = key0 + kBlock <= last_key;
-        if (c.t_log2 > 4) {             // (a step's blocks share a page)
-            w.ok[1] = w.ok[0] && wanted;
-            w.k[1] = w.k[0] + kBlock * HD;
-            w.e[1] = w.e[0] + 2;
-        } else block(1, wanted ? ids.get((key0 + kBlock) >> c.t_log2) : -1, wanted);
+        }
         return w;
     }
     static __device__ __forceinline__ void load_k(const Where<HD>& w, Step<HD>& s)
@@ -215,6 +217,47 @@ struct Attention {
 
     struct Scores { f32x4 s[2][NT]; };
     static constexpr bool kSharedQ = NT >= 4;   // Q's fragments in LDS (the waves have the same rows): 64 registers less
+    // Prompts with head_dim 128: K's codes are the operand themselves, with their block's exponent as the matrix instruction's scale, and a row of Q
+    // is two rows of codes under one exponent e: q = 2^e (high + low / 16).  A bf16 value's eight bits are a four-bit high part and a four-bit
+    // remainder, so the split is exact down to 2^-22 of the row's largest element; two 16 x 16 x 128 products take what four
+    // bf16 ones take, without the conversion of K.
+    static constexpr bool kCodesQ = kSharedQ && HD == 128;
+    typedef __attribute__((ext_vector_type(8))) int i32x8;
+
+    static __device__ __forceinline__ void split_q(const u32x4 (&w)[4], u32x4 (&high)[2], u32x4 (&low)[2], unsigned int& exponents)
+    {
+        float x[32], amax = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) unpack8(w[i], x + 8 * i);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) amax = fmaxf(amax, fabsf(x[i]));
+        amax = column_max(amax);                                       // (an infinity is 448 and more: its code is made NaN below)
+        const unsigned int u = __float_as_uint(fminf(amax, 3e38f));
+        const int e = min(max((int)(u >> 23) - 127 - ((u & 0x7fffffu) <= 0x600000u ? 8 : 7), -100), 119);   // least with amax <= 448 * 2^e
+        const float r = __uint_as_float((unsigned)(127 - e) << 23);
+        exponents = (unsigned)(e + 127) | (unsigned)(e + 123) << 8;    // E8M0: of high, of low
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            unsigned int hi = 0, lo = 0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float a[2], rest[2];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const float v = x[4 * i + 2 * h + k];
+                    a[k] = fabsf(v) < __builtin_inff() ? fminf(fmaxf(v * r, -448.f), 448.f) : __builtin_nanf("");
+                }
+                const unsigned int code = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(a[0], a[1], 0, false) & 0xffffu;
+                const f32x2 back = __builtin_amdgcn_cvt_pk_f32_fp8((int)code, false);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) rest[k] = (a[k] - back[k]) * 16.f;
+                hi |= code << (16 * h);
+                lo |= ((unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(rest[0], rest[1], 0, false) & 0xffffu) << (16 * h);
+            }
+            high[i / 4][i % 4] = hi;
+            low[i / 4][i % 4] = lo;
+        }
+    }
 
     static __device__ __forceinline__ void scores(const Step<HD>& s, const bf16x8 (&q)[kSharedQ ? 1 : NT][HD / 32], const Shared& sh, Scores& sc)
     {
@@ -223,30 +266,98 @@ struct Attention {
 #pragma unroll
             for (int n = 0; n < NT; ++n) sc.s[b][n] = f32x4{0.f, 0.f, 0.f, 0.f};
         if constexpr (kSharedQ) asm volatile("" ::: "memory");   // (read again every step: kept in registers, Q would displace the sums)
-        const float k0 = block_scale(s.e[0] & 0xffu), k1 = block_scale(s.e[1] & 0xffu);
+        const float k0 = block_scale(uniform((int)s.e[0]) & 0xffu), k1 = block_scale(uniform((int)s.e[1]) & 0xffu);
         u32x4 k[2][LD];
         operand_k(s.k[0], k[0]);
         operand_k(s.k[1], k[1]);
+        if constexpr (kCodesQ) {
+            i32x8 a[2];
 #pragma unroll
-        for (int j = 0; j < LD; ++j)
+            for (int b = 0; b < 2; ++b)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const bf16x8 a0 = h == 0 ? eight_bf16(k[0][j].x, k0, k[0][j].y, k0) : eight_bf16(k[0][j].z, k0, k[0][j].w, k0);
-                const bf16x8 a1 = h == 0 ? eight_bf16(k[1][j].x, k1, k[1][j].y, k1) : eight_bf16(k[1][j].z, k1, k[1][j].w, k1);
+                for (int i = 0; i < 8; ++i) a[b][i] = (int)k[b][i / 4][i % 4];
+            const int e0 = uniform((int)s.e[0]) & 0xff, e1 = uniform((int)s.e[1]) & 0xff;
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    bf16x8 qf;
-                    if constexpr (kSharedQ) qf = __builtin_bit_cast(bf16x8, sh.q[n][2 * j + h][lane_id()]);
-                    else qf = q[n][2 * j + h];
-                    sc.s[0][n] = mfma(a0, qf, sc.s[0][n]);
-                    sc.s[1][n] = mfma(a1, qf, sc.s[1][n]);
+            for (int n = 0; n < NT; ++n) {
+                const int qe = (int)sh.q_exp[n][lane_id() & 15];
+#pragma unroll
+                for (int part = 0; part < 2; ++part) {
+                    i32x8 qf;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const u32x4 w = sh.q[n][2 * part + i][lane_id()];
+                        qf[4 * i] = (int)w.x; qf[4 * i + 1] = (int)w.y; qf[4 * i + 2] = (int)w.z; qf[4 * i + 3] = (int)w.w;
+                    }
+                    if (part == 0) {
+                        sc.s[0][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a[0], qf, sc.s[0][n], 0, 0, 0, e0, 0, qe);
+                        sc.s[1][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a[1], qf, sc.s[1][n], 0, 0, 0, e1, 0, qe);
+                    } else {
+                        sc.s[0][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a[0], qf, sc.s[0][n], 0, 0, 0, e0, 1, qe);
+                        sc.s[1][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a[1], qf, sc.s[1][n], 0, 0, 0, e1, 1, qe);
+                    }
                 }
             }
+            pace<3>();
+            return;
+        }
+        bf16x8 a[2][HD / 32];
+#pragma unroll
+        for (int j = 0; j < LD; ++j) {
+            a[0][2 * j] = eight_bf16(k[0][j].x, k0, k[0][j].y, k0);
+            a[1][2 * j] = eight_bf16(k[1][j].x, k1, k[1][j].y, k1);
+            a[0][2 * j + 1] = eight_bf16(k[0][j].z, k0, k[0][j].w, k0);
+            a[1][2 * j + 1] = eight_bf16(k[1][j].z, k1, k[1][j].w, k1);
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int g = 0; g < HD / 32; ++g) {
+                bf16x8 qf;
+                if constexpr (kSharedQ) qf = __builtin_bit_cast(bf16x8, sh.q[n][g][lane_id()]);
+                else qf = q[n][g];
+                sc.s[0][n] = mfma(a[0][g], qf, sc.s[0][n]);
+                sc.s[1][n] = mfma(a[1][g], qf, sc.s[1][n]);
+            }
+        pace<3>();
     }
+
+    // Fragments of Q from LDS: the first AHEAD on their way before the first products, then as many reads as a pair of products needs behind it
+    // (left alone, the reads are either all in front, which takes registers that spill, or each waited for).
+    template <int AHEAD>
+    static __device__ __forceinline__ void pace()
+    {
+        if constexpr (kSharedQ) {
+            constexpr int PER = kCodesQ ? 2 : 1, PAIRS = NT * HD / 32 / PER;        // reads of a pair; pairs of products
+            __builtin_amdgcn_sched_group_barrier(0x100, AHEAD * PER, 0);           // LDS reads
+#pragma unroll
+            for (int i = 0; i < PAIRS - AHEAD; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x8, 2, 0);                    // matrix products
+                __builtin_amdgcn_sched_group_barrier(0x100, PER, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x8, 2 * AHEAD, 0);
+        }
+    }
+
+    // The rows of a tile: row row_base + x is query head y % group of token token0 + y / group, y = within0 + x.
+    struct Rows {
+        int token0, within0, left, first, group;    // left: rows from row_base on
+        unsigned int magic;
+        __device__ __forceinline__ int token(int x) const { return token0 + (int)(((unsigned)(within0 + x) * magic) >> 20); }
+        __device__ __forceinline__ int query(int x) const { return within0 + x - (token(x) - token0) * group; }
+        // the last position that the lane's rows see; -1: no row
+        __device__ __forceinline__ void limits(int (&limit)[NT]) const
+        {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const int x = 16 * n + (lane_id() & 15);
+                limit[n] = x < left ? first + token(x) : -1;
+            }
+        }
+    };
 
     // probabilities of a step, and its share of O^T
     static __device__ __forceinline__ void accumulate(const u32x4 (&v)[2][LD], bool ok0, bool ok1, Scores& scores, const unsigned int (&e)[2],
-                                                      const int (&limit)[NT], int key0, int last_key, bool masked, float c_log2, State& st)
+                                                      const Rows& rows, int key0, int last_key, bool masked, float c_log2, State& st)
     {
         const bool ok[2] = {ok0, ok1};
         const int kg = lane_id() >> 4;
@@ -257,6 +368,9 @@ struct Attention {
 #pragma unroll
             for (int i = 0; i < D; ++i) vw[b][i] = v[b][i / 4][i % 4];
         if (masked) {
+            asm volatile("" ::: "memory");      // (a branch: selected without one, every step would pay for it)
+            int limit[NT];
+            rows.limits(limit);
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 const int key = key0 + b * kBlock + 4 * kg;
@@ -296,21 +410,8 @@ struct Attention {
                     for (int r = 0; r < 4; ++r) st.o[n][i][r] *= a;
             }
         }
-        bf16x8 pt[NT];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const float m = st.m[n] == -__builtin_inff() ? 0.f : st.m[n];   // (nothing seen yet: 2^-inf = 0)
-            float e[8], sum = 0.f;
-#pragma unroll
-            for (int r = 0; r < 8; ++r) {
-                e[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[r / 4][n][r % 4], c_log2, -m));
-                sum += e[r];
-            }
-            st.l[n] += sum;
-            // bf16 probabilities (rounded: 2^-9 of a term on average in the sum of p v, below the output's own rounding)
-            pt[n] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7])});
-        }
         if (masked) {
+            asm volatile("" ::: "memory");
             // 0 x NaN is NaN: a NaN value must reach the rows that see its position and no others
             unsigned int nan = 0;
 #pragma unroll
@@ -319,6 +420,8 @@ struct Attention {
                 for (int i = 0; i < D; ++i) nan |= ((vw[b][i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
             if (__any(nan != 0)) {
                 unsigned int seen[NT][4];
+                int limit[NT];
+                rows.limits(limit);
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -346,12 +449,25 @@ struct Attention {
                 }
             }
         }
-        const float v0 = ok[0] ? block_scale(e[0] >> 8) : 1.f, v1 = ok[1] ? block_scale(e[1] >> 8) : 1.f;
+        const float v0 = ok[0] ? block_scale((unsigned)uniform((int)e[0]) >> 8) : 1.f, v1 = ok[1] ? block_scale((unsigned)uniform((int)e[1]) >> 8) : 1.f;
+        bf16x8 vt[D];
 #pragma unroll
-        for (int i = 0; i < D; ++i) {
-            const bf16x8 a = eight_bf16(vw[0][i], v0, vw[1][i], v1);
+        for (int i = 0; i < D; ++i) vt[i] = eight_bf16(vw[0][i], v0, vw[1][i], v1);
+        // (row tile by row tile: the matrix products of one run beside the exponentials of the next)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) st.o[n][i] = mfma(a, pt[n], st.o[n][i]);
+        for (int n = 0; n < NT; ++n) {
+            const float m = st.m[n] == -__builtin_inff() ? 0.f : st.m[n];   // (nothing seen yet: 2^-inf = 0)
+            float x[8], sum = 0.f;
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[r / 4][n][r % 4], c_log2, -m));
+                sum += x[r];
+            }
+            st.l[n] += sum;
+            // bf16 probabilities (rounded: 2^-9 of a term on average in the sum of p v, below the output's own rounding)
+            const bf16x8 pt = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])});
+#pragma unroll
+            for (int i = 0; i < D; ++i) st.o[n][i] = mfma(vt[i], pt, st.o[n][i]);
         }
     }
 
@@ -363,37 +479,54 @@ struct Attention {
         const int last_row = min(row_base + 16 * NT, rows) - 1;
         const int last_key = u.first + last_row / p.group;                        // the last position that a row of the tile sees
         const int begin = u.chunk * chunk_len, end = min(begin + chunk_len, last_key + 1);
-        const int token0 = row_base / p.group, within0 = row_base - token0 * p.group;
-        const int first_pos = u.first + token0;                                   // the first row's
-        // token and query head of row row_base + x of the tile
+        Rows tr;
+        tr.token0 = row_base / p.group;
+        tr.within0 = row_base - tr.token0 * p.group;
+        tr.left = rows - row_base;
+        tr.first = u.first;
+        tr.group = p.group;
+        tr.magic = p.group_magic;
+        const int first_pos = u.first + tr.token0;                                // the first row's
         const auto row_of = [&](int x, int& token, int& h) {
-            const int y = within0 + x, t = (int)(((unsigned)y * p.group_magic) >> 20);
-            token = token0 + t;
-            h = u.head * p.group + y - t * p.group;
+            token = tr.token(x);
+            h = u.head * p.group + tr.query(x);
         };
-
         bf16x8 q[kSharedQ ? 1 : NT][HD / 32];
-        int limit[NT];
         State st;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const int r = row_base + 16 * n + col;
             int token, h;
             row_of(16 * n + col, token, h);
-            limit[n] = r < rows ? u.first + token : -1;
             st.m[n] = -__builtin_inff();
             st.l[n] = 0.f;
 #pragma unroll
             for (int i = 0; i < D; ++i) st.o[n][i] = f32x4{0.f, 0.f, 0.f, 0.f};
             if (kSharedQ && n % kAttnWaves != wave) continue;
             const u16* src = p.q + (long long)(u.row0 + token) * p.ldq + h * HD + kg * 16;
+            u32x4 w[HD / 32];
 #pragma unroll
             for (int j = 0; j < HD / 32; ++j) {
-                u32x4 w{0, 0, 0, 0};
-                if (r < rows) w = *reinterpret_cast<const u32x4*>(src + (j / 2) * 64 + (j % 2) * 8);
-                w.x ^= p.q_sign; w.y ^= p.q_sign; w.z ^= p.q_sign; w.w ^= p.q_sign;
-                if constexpr (kSharedQ) sh.q[n][j][lane] = w;
-                else q[n][j] = __builtin_bit_cast(bf16x8, w);
+                w[j] = u32x4{0, 0, 0, 0};
+                if (r < rows) w[j] = *reinterpret_cast<const u32x4*>(src + (j / 2) * 64 + (j % 2) * 8);
+                w[j].x ^= p.q_sign; w[j].y ^= p.q_sign; w[j].z ^= p.q_sign; w[j].w ^= p.q_sign;
+            }
+            if constexpr (kCodesQ) {
+                u32x4 high[2], low[2];
+                unsigned int exponents;
+                split_q(w, high, low, exponents);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    sh.q[n][i][lane] = high[i];
+                    sh.q[n][2 + i][lane] = low[i];
+                }
+                if (kg == 0) sh.q_exp[n][col] = exponents;
+            } else {
+#pragma unroll
+                for (int j = 0; j < HD / 32; ++j) {
+                    if constexpr (kSharedQ) sh.q[n][j][lane] = w[j];
+                    else q[n][j] = __builtin_bit_cast(bf16x8, w[j]);
+                }
             }
         }
         if (kSharedQ) __syncthreads();
@@ -403,7 +536,8 @@ struct Attention {
             PageIds ids;
             ids.start(c.table + (long long)u.slot * c.max_pages, (last_key >> c.t_log2) + 1, key >> c.t_log2);
             Step<HD> s;
-            Where<HD> w = find_step(p, ids, u, key, last_key);
+            bool bad = false;
+            Where<HD> w = find_step(p, ids, u, key, last_key, bad);
             load_k(w, s);
             load_v(p, w, s);
             const auto is_masked = [&](const Step<HD>& t) { return key + kStep - 1 > first_pos || !t.ok[0] || !t.ok[1]; };
@@ -412,13 +546,15 @@ struct Attention {
                 // same codes are requested again: no branch)
                 for (; key < end; key += kRound) {
                     const int next = key + kRound < end ? key + kRound : key;
-                    Scores sc;
-                    scores(s, q, sh, sc);
                     const bool masked = is_masked(s), ok0 = s.ok[0], ok1 = s.ok[1];
-                    const unsigned int e[2] = {s.e[0], s.e[1]};
-                    w = find_step(p, ids, u, next, last_key);
+                    const unsigned int e[2] = {(unsigned)uniform((int)s.e[0]), (unsigned)uniform((int)s.e[1])};
+                    w = find_step(p, ids, u, next, last_key, bad);
+                    Scores sc;
+                    __builtin_amdgcn_s_setprio(1);      // (the other wave of the SIMD has exponentials to do)
+                    scores(s, q, sh, sc);
+                    __builtin_amdgcn_s_setprio(0);
                     load_k(w, s);
-                    accumulate(s.v, ok0, ok1, sc, e, limit, key, last_key, masked, p.c_log2, st);
+                    accumulate(s.v, ok0, ok1, sc, e, tr, key, last_key, masked, p.c_log2, st);
                     load_v(p, w, s);
                 }
             } else {
@@ -427,18 +563,19 @@ struct Attention {
                     const int next = key + kRound;
                     Step<HD> ahead = s;
                     if (next < end) {
-                        w = find_step(p, ids, u, next, last_key);
+                        w = find_step(p, ids, u, next, last_key, bad);
                         load_k(w, ahead);
                         load_v(p, w, ahead);
                     }
                     Scores sc;
                     scores(s, q, sh, sc);
-                    accumulate(s.v, s.ok[0], s.ok[1], sc, s.e, limit, key, last_key, is_masked(s), p.c_log2, st);
+                    accumulate(s.v, s.ok[0], s.ok[1], sc, s.e, tr, key, last_key, is_masked(s), p.c_log2, st);
                     if (next >= end) break;
                     key = next;
                     s = ahead;
                 }
             }
+            if (bad && lane == 0) atomicOr(c.err, kErrBadSegment);
         }
         if (kSharedQ) __syncthreads();          // acc takes q's place
 
@@ -528,7 +665,7 @@ struct Attention {
             __syncthreads();
             for (int i = (int)threadIdx.x; i < u.chunks << row_log2; i += kAttnThreads)
                 if ((i & mask) < live)
-                    sh.ml[i] = __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(part, stat_at + (16 * n + (i & mask)) * 8, (u.slot0 + (i >> row_log2)) * slot_bytes, kSc1));
+                    sh.ml[i] = __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(part, stat_at + (16 * n + (i & mask)) * 8 + (u.slot0 + (i >> row_log2)) * slot_bytes, 0, kSc1));
             __syncthreads();
             // sixteen threads a row: its maximum, its sum, and every chunk's factor
             const int row = (int)threadIdx.x / 16, j = (int)threadIdx.x % 16;
@@ -556,11 +693,11 @@ struct Attention {
             if (r < live) {
 #pragma unroll 2
                 for (int k = group; k < u.chunks; k += groups) {
-                    const int at = (u.slot0 + k) * slot_bytes;
+                    const int at = (u.slot0 + k) * slot_bytes + row_bytes(r);
                     const float a = sh.ml[(k << row_log2) + r].x;
 #pragma unroll
                     for (int i = 0; i < D; i += 4) {
-                        const f32x4 v = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(part, row_bytes(r) + (out_col + i) * 4, at, kSc1));
+                        const f32x4 v = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(part, at + (out_col + i) * 4, 0, kSc1));
 #pragma unroll
                         for (int x = 0; x < 4; ++x) o[i + x] += v[x] * a;
                     }
