@@ -35,7 +35,9 @@ constexpr int kLeastChunk = 2 * kRound;
 constexpr int kClasses = 5;
 constexpr int kKeptSpans = 1024;                // spans that a workgroup keeps in LDS (16 KB); of more, a unit's is read again
 __host__ __device__ constexpr int span_at(int n) { return (3 * n + 1 + 3) / 4 * 4; }
+constexpr float kNone = -3e38f;                 // a maximum before anything was seen: below every score, and finite (no case of its own anywhere)
 constexpr float kLazy = 8.f;                    // log2 of how far a score may exceed the maximum that its exponentials use
+constexpr int kAllButOrder = 0x4;              // what the scheduler may move across: scalar arithmetic
 constexpr int kRawBuffer = 0x00020000, kSc1 = 16;   // descriptor word 3 (raw 32-bit data); device-scope cache policy
 
 struct AttnParams {
@@ -144,7 +146,7 @@ struct Attention {
             float acc[kAttnWaves][16][PITCH];
             struct {
                 u32x4 q[NT][HD / 32][kWave];    // fragments: of bf16 values; or of codes, high parts and low parts
-                unsigned int q_exp[NT][16];
+                uint8_t q_exp[16][4];
             };
             f32x2 ml[256 * 16];                 // of a split tile's chunks: maxima (then factors) and sums
         };
@@ -156,23 +158,22 @@ struct Attention {
 
     // The addresses of a step's two blocks (their entries lie in one batch: a step begins at a multiple of 32 positions).  A block that is
     // not there gets page 0's: what is read is not used.  bad: whether a position that a row sees has no usable page.
-    static __device__ __forceinline__ Where<HD> find_step(const AttnParams& p, PageIds& ids, const Unit& u, int key0, int last_key, bool& bad)
+    struct Head { const uint8_t* k; const uint8_t* e; unsigned int page_bytes, n_pages; int t_log2; };   // of page 0: the unit's key head
+    static __device__ __forceinline__ Where<HD> find_step(const Head& hd, PageIds& ids, int key0, int last_key, bool& bad)
     {
-        const CacheView& c = p.c;
-        const int T = 1 << c.t_log2;
         Where<HD> w;
-        ids.reach(key0 >> c.t_log2);
+        ids.reach(key0 >> hd.t_log2);
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-            const int key = key0 + b * kBlock, in = key & (T - 1);
-            const bool wanted = key <= last_key;
-            const int page = ids.get(min(key, last_key) >> c.t_log2);
-            const bool usable = page >= 0 && page < c.n_pages;
+            const int key = key0 + b * kBlock;
+            const unsigned int in = (unsigned)key & ((1u << hd.t_log2) - 1u);
+            const unsigned int page = (unsigned)ids.get(min(key, last_key) >> hd.t_log2);
+            const bool usable = page < hd.n_pages;
             bad = bad || !usable;
-            w.ok[b] = usable && wanted;
-            const uint8_t* at = p.pages + (usable ? page : 0) * c.page_bytes;
-            w.k[b] = at + (u.head * 2 * T + in) * HD;
-            w.e[b] = at + c.scale_off + (u.head * (T / kBlock) + in / kBlock) * 2;
+            w.ok[b] = usable && key <= last_key;
+            const unsigned long long at = (unsigned long long)(usable ? page : 0u) * hd.page_bytes;
+            w.k[b] = hd.k + (at + in * HD);
+            w.e[b] = hd.e + (at + in / kBlock * 2);
         }
         return w;
     }
@@ -223,8 +224,9 @@ struct Attention {
     // bf16 ones take, without the conversion of K.
     static constexpr bool kCodesQ = kSharedQ && HD == 128;
     typedef __attribute__((ext_vector_type(8))) int i32x8;
+    static constexpr int kAhead = 3;
 
-    static __device__ __forceinline__ void split_q(const u32x4 (&w)[4], u32x4 (&high)[2], u32x4 (&low)[2], unsigned int& exponents)
+    static __device__ __forceinline__ void split_q(const u32x4 (&w)[4], u32x4 (&high)[2], u32x4 (&low)[2], unsigned int& exponent)
     {
         float x[32], amax = 0.f;
 #pragma unroll
@@ -235,7 +237,7 @@ struct Attention {
         const unsigned int u = __float_as_uint(fminf(amax, 3e38f));
         const int e = min(max((int)(u >> 23) - 127 - ((u & 0x7fffffu) <= 0x600000u ? 8 : 7), -100), 119);   // least with amax <= 448 * 2^e
         const float r = __uint_as_float((unsigned)(127 - e) << 23);
-        exponents = (unsigned)(e + 127) | (unsigned)(e + 123) << 8;    // E8M0: of high, of low
+        exponent = (unsigned)(e + 127);                                // E8M0, of the high parts; the low parts' is 4 less
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             unsigned int hi = 0, lo = 0;
@@ -259,7 +261,17 @@ struct Attention {
         }
     }
 
-    static __device__ __forceinline__ void scores(const Step<HD>& s, const bf16x8 (&q)[kSharedQ ? 1 : NT][HD / 32], const Shared& sh, Scores& sc)
+    // n: the byte of qe that holds the exponents of row tile n (a constant once the loops are unrolled)
+    static __device__ __forceinline__ f32x4 mfma_codes(int n, i32x8 a, i32x8 b, f32x4 c, int ke, int qe)
+    {
+        return n == 0   ? __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, ke, 0, qe)
+               : n == 1 ? __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, ke, 1, qe)
+               : n == 2 ? __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, ke, 2, qe)
+                        : __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, ke, 3, qe);
+    }
+
+    // q_exp: with kCodesQ, the exponents of the lane's row in the row tiles, a byte each
+    static __device__ __forceinline__ void scores(const Step<HD>& s, const bf16x8 (&q)[kSharedQ ? 1 : NT][HD / 32], int q_exp, const Shared& sh, Scores& sc)
     {
 #pragma unroll
         for (int b = 0; b < 2; ++b)
@@ -277,27 +289,25 @@ struct Attention {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) a[b][i] = (int)k[b][i / 4][i % 4];
             const int e0 = uniform((int)s.e[0]) & 0xff, e1 = uniform((int)s.e[1]) & 0xff;
+            const int low_exp = q_exp - 0x04040404;
+            const auto fragment = [&](int i) {      // of row tile i / 2: its high parts, its low parts
+                const u32x4 x = sh.q[i / 2][i % 2 * 2][lane_id()], y = sh.q[i / 2][i % 2 * 2 + 1][lane_id()];
+                return i32x8{(int)x.x, (int)x.y, (int)x.z, (int)x.w, (int)y.x, (int)y.y, (int)y.z, (int)y.w};
+            };
+            // kAhead fragments on their way while a pair of products runs (in this order: left to the scheduler, the reads are either all in
+            // front, which takes registers that spill, or each is waited for)
+            i32x8 f[kAhead + 1];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const int qe = (int)sh.q_exp[n][lane_id() & 15];
+            for (int i = 0; i < kAhead; ++i) f[i] = fragment(i);
 #pragma unroll
-                for (int part = 0; part < 2; ++part) {
-                    i32x8 qf;
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const u32x4 w = sh.q[n][2 * part + i][lane_id()];
-                        qf[4 * i] = (int)w.x; qf[4 * i + 1] = (int)w.y; qf[4 * i + 2] = (int)w.z; qf[4 * i + 3] = (int)w.w;
-                    }
-                    if (part == 0) {
-                        sc.s[0][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a[0], qf, sc.s[0][n], 0, 0, 0, e0, 0, qe);
-                        sc.s[1][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a[1], qf, sc.s[1][n], 0, 0, 0, e1, 0, qe);
-                    } else {
-                        sc.s[0][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a[0], qf, sc.s[0][n], 0, 0, 0, e0, 1, qe);
-                        sc.s[1][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a[1], qf, sc.s[1][n], 0, 0, 0, e1, 1, qe);
-                    }
-                }
+            for (int i = 0; i < 2 * NT; ++i) {
+                if (i + kAhead < 2 * NT) f[(i + kAhead) % (kAhead + 1)] = fragment(i + kAhead);
+                __builtin_amdgcn_sched_barrier(0);
+                const int qe = i % 2 == 0 ? q_exp : low_exp;
+                sc.s[0][i / 2] = mfma_codes(i / 2, a[0], f[i % (kAhead + 1)], sc.s[0][i / 2], e0, qe);
+                sc.s[1][i / 2] = mfma_codes(i / 2, a[1], f[i % (kAhead + 1)], sc.s[1][i / 2], e1, qe);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            pace<3>();
             return;
         }
         bf16x8 a[2][HD / 32];
@@ -356,7 +366,9 @@ struct Attention {
     };
 
     // probabilities of a step, and its share of O^T
-    static __device__ __forceinline__ void accumulate(const u32x4 (&v)[2][LD], bool ok0, bool ok1, Scores& scores, const unsigned int (&e)[2],
+    // request() is called halfway, when half of the scores' registers are free
+    template <class Request>
+    static __device__ __forceinline__ void accumulate(Request&& request, const u32x4 (&v)[2][LD], bool ok0, bool ok1, Scores& scores, const unsigned int (&e)[2],
                                                       const Rows& rows, int key0, int last_key, bool masked, float c_log2, State& st)
     {
         const bool ok[2] = {ok0, ok1};
@@ -401,7 +413,7 @@ struct Attention {
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const float m = fmaxf(st.m[n], column_max(top[n]) * c_log2);
-                const float a = m == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(st.m[n] - m);
+                const float a = __builtin_amdgcn_exp2f(st.m[n] - m);
                 st.m[n] = m;
                 st.l[n] *= a;
 #pragma unroll
@@ -453,21 +465,43 @@ struct Attention {
         bf16x8 vt[D];
 #pragma unroll
         for (int i = 0; i < D; ++i) vt[i] = eight_bf16(vw[0][i], v0, vw[1][i], v1);
-        // (row tile by row tile: the matrix products of one run beside the exponentials of the next)
+        // Row tile by row tile, the products of one between the exponentials of the next, in this order: a product occupies its unit
+        // for four vector instructions' time, and left alone the scheduler puts the products, and the exponentials, in a row.
+        constexpr int PER = 8 / D;                  // exponentials between two products
+        float x[2][8], sum[2];
+        u32x4 pt[2];
+        const auto exponential = [&](int n, int r) { x[n % 2][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[r / 4][n][r % 4], c_log2, -st.m[n])); };
+        // (bf16 probabilities: rounded, 2^-9 of a term on average in the sum of p v, below the output's own rounding)
+        const auto pack = [&](int n, int r) { pt[n % 2][r / 2] = pack_bf16x2(x[n % 2][r], x[n % 2][r + 1]); };
+        const auto add = [&](int n, int r) { sum[n % 2] = r == 0 ? x[n % 2][0] : sum[n % 2] + x[n % 2][r]; };
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            exponential(0, r);
+            if (r % 2) pack(0, r - 1);
+            add(0, r);
+        }
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const float m = st.m[n] == -__builtin_inff() ? 0.f : st.m[n];   // (nothing seen yet: 2^-inf = 0)
-            float x[8], sum = 0.f;
+            st.l[n] += sum[n % 2];
+            const bf16x8 p = __builtin_bit_cast(bf16x8, pt[n % 2]);
 #pragma unroll
-            for (int r = 0; r < 8; ++r) {
-                x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[r / 4][n][r % 4], c_log2, -m));
-                sum += x[r];
+            for (int i = 0; i < D; ++i) {
+                st.o[n][i] = mfma(vt[i], p, st.o[n][i]);
+                if (n + 1 < NT) {
+#pragma unroll
+                    for (int r = i * PER; r < (i + 1) * PER; ++r) {
+                        exponential(n + 1, r);
+                        if (r > 0) add(n + 1, r - 1);
+                        if (r > 1 && r % 2 == 0) pack(n + 1, r - 2);
+                    }
+                    __builtin_amdgcn_sched_barrier(kAllButOrder);
+                }
             }
-            st.l[n] += sum;
-            // bf16 probabilities (rounded: 2^-9 of a term on average in the sum of p v, below the output's own rounding)
-            const bf16x8 pt = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])});
-#pragma unroll
-            for (int i = 0; i < D; ++i) st.o[n][i] = mfma(vt[i], pt, st.o[n][i]);
+            if (n + 1 < NT) {
+                add(n + 1, 7);
+                pack(n + 1, 6);
+            }
+            if (n == NT / 2 - 1) request();
         }
     }
 
@@ -498,7 +532,7 @@ struct Attention {
             const int r = row_base + 16 * n + col;
             int token, h;
             row_of(16 * n + col, token, h);
-            st.m[n] = -__builtin_inff();
+            st.m[n] = kNone;
             st.l[n] = 0.f;
 #pragma unroll
             for (int i = 0; i < D; ++i) st.o[n][i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -513,14 +547,14 @@ struct Attention {
             }
             if constexpr (kCodesQ) {
                 u32x4 high[2], low[2];
-                unsigned int exponents;
-                split_q(w, high, low, exponents);
+                unsigned int exponent;
+                split_q(w, high, low, exponent);
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     sh.q[n][i][lane] = high[i];
                     sh.q[n][2 + i][lane] = low[i];
                 }
-                if (kg == 0) sh.q_exp[n][col] = exponents;
+                if (kg == 0) sh.q_exp[col][n] = (uint8_t)exponent;
             } else {
 #pragma unroll
                 for (int j = 0; j < HD / 32; ++j) {
@@ -530,6 +564,7 @@ struct Attention {
             }
         }
         if (kSharedQ) __syncthreads();
+        const int q_exp = kCodesQ ? *reinterpret_cast<const int*>(sh.q_exp[col]) : 0;
 
         int key = begin + wave * kStep;
         if (key < end) {
@@ -537,7 +572,10 @@ struct Attention {
             ids.start(c.table + (long long)u.slot * c.max_pages, (last_key >> c.t_log2) + 1, key >> c.t_log2);
             Step<HD> s;
             bool bad = false;
-            Where<HD> w = find_step(p, ids, u, key, last_key, bad);
+            const int T = 1 << c.t_log2;
+            const Head hd{p.pages + (long long)u.head * 2 * T * HD, p.pages + c.scale_off + u.head * (T / kBlock) * 2, (unsigned)c.page_bytes,
+                          (unsigned)c.n_pages, c.t_log2};
+            Where<HD> w = find_step(hd, ids, key, last_key, bad);
             load_k(w, s);
             load_v(p, w, s);
             const auto is_masked = [&](const Step<HD>& t) { return key + kStep - 1 > first_pos || !t.ok[0] || !t.ok[1]; };
@@ -548,13 +586,12 @@ struct Attention {
                     const int next = key + kRound < end ? key + kRound : key;
                     const bool masked = is_masked(s), ok0 = s.ok[0], ok1 = s.ok[1];
                     const unsigned int e[2] = {(unsigned)uniform((int)s.e[0]), (unsigned)uniform((int)s.e[1])};
-                    w = find_step(p, ids, u, next, last_key, bad);
+                    w = find_step(hd, ids, next, last_key, bad);
                     Scores sc;
                     __builtin_amdgcn_s_setprio(1);      // (the other wave of the SIMD has exponentials to do)
-                    scores(s, q, sh, sc);
+                    scores(s, q, q_exp, sh, sc);
                     __builtin_amdgcn_s_setprio(0);
-                    load_k(w, s);
-                    accumulate(s.v, ok0, ok1, sc, e, tr, key, last_key, masked, p.c_log2, st);
+                    accumulate([&] { load_k(w, s); }, s.v, ok0, ok1, sc, e, tr, key, last_key, masked, p.c_log2, st);
                     load_v(p, w, s);
                 }
             } else {
@@ -563,13 +600,13 @@ struct Attention {
                     const int next = key + kRound;
                     Step<HD> ahead = s;
                     if (next < end) {
-                        w = find_step(p, ids, u, next, last_key, bad);
+                        w = find_step(hd, ids, next, last_key, bad);
                         load_k(w, ahead);
                         load_v(p, w, ahead);
                     }
                     Scores sc;
-                    scores(s, q, sh, sc);
-                    accumulate(s.v, s.ok[0], s.ok[1], sc, s.e, tr, key, last_key, is_masked(s), p.c_log2, st);
+                    scores(s, q, q_exp, sh, sc);
+                    accumulate([] {}, s.v, s.ok[0], s.ok[1], sc, s.e, tr, key, last_key, is_masked(s), p.c_log2, st);
                     if (next >= end) break;
                     key = next;
                     s = ahead;
@@ -598,7 +635,7 @@ struct Attention {
             float top = sh.m[0][16 * n + col];
 #pragma unroll
             for (int w = 1; w < kAttnWaves; ++w) top = fmaxf(top, sh.m[w][16 * n + col]);
-            const float a = st.m[n] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(st.m[n] - top);
+            const float a = __builtin_amdgcn_exp2f(st.m[n] - top);
 #pragma unroll
             for (int i4 = 0; i4 < D / 4; ++i4)
 #pragma unroll
@@ -615,7 +652,7 @@ struct Attention {
 #pragma unroll
                 for (int w = 0; w < kAttnWaves; ++w) {
                     const float mw = sh.m[w][16 * n + out_row];
-                    l += mw == -__builtin_inff() ? 0.f * sh.l[w][16 * n + out_row] : sh.l[w][16 * n + out_row] * __builtin_amdgcn_exp2f(mw - mt);
+                    l += sh.l[w][16 * n + out_row] * __builtin_amdgcn_exp2f(mw - mt);
                 }
                 float o[D];
 #pragma unroll
@@ -670,13 +707,13 @@ struct Attention {
             // sixteen threads a row: its maximum, its sum, and every chunk's factor
             const int row = (int)threadIdx.x / 16, j = (int)threadIdx.x % 16;
             if (row < live) {
-                float top = -__builtin_inff(), l = 0.f;
+                float top = kNone, l = 0.f;
                 for (int k = j; k < u.chunks; k += 16) top = fmaxf(top, sh.ml[(k << row_log2) + row].x);
 #pragma unroll
                 for (int d = 1; d < 16; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, kWave));
                 for (int k = j; k < u.chunks; k += 16) {
                     f32x2& ml = sh.ml[(k << row_log2) + row];
-                    const float a = ml.x == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
+                    const float a = __builtin_amdgcn_exp2f(ml.x - top);
                     l += ml.y * a;
                     ml.x = a;
                 }
