@@ -45,43 +45,55 @@ constexpr int kMaxPageTokens = 256;
 // A span's blocks are found without a table of them: span s owns the items from row_starts[s] / 16 + 2 s on, which are enough
 // for n rows at any offset (at most (n + 14) / 16 + 1 blocks); the others have nothing to do.
 // =================================================================================================
-struct BlockJob { int row0, n, first, pos0; const uint8_t* page; int in_page; bool ok; };  // pos0: first position of the block
+// A wave's start is a chain of dependent round trips (spans, span, table and rows, page); nothing of a trip waits for a check of the one
+// before: indexes are brought into range instead, and what was found is looked at when all of it is there.
+struct BlockJob { int slot, row0, n, first, pos0, page, len; bool rows_ok; };  // pos0: first position of the block
 
-template <bool STORE>
-__device__ __forceinline__ BlockJob find_block(const CacheView& c, const Spans& sp, const uint8_t* pages, int item)
+// span and block of an item, with its length and page requested; false: nothing to do
+__device__ __forceinline__ bool find_block(const CacheView& c, const Spans& sp, int item, BlockJob& j)
 {
-    BlockJob j;
-    j.ok = false;
-    const int s = last_not_above(sp.n_seqs, item, [&](int k) { return (sp.row_starts[k] >> 4) + 2 * k; });
-    if (s < 0) return j;
-    const Span u = load_span(c, sp, s);
-    const int local = item - ((u.row0 >> 4) + 2 * s);
-    if (u.n <= 0 || local < 0 || local > ((u.first + u.n - 1) >> 4) - (u.first >> 4)) return j;
-    j.row0 = u.row0;
-    j.n = u.n;
-    j.first = u.first;
-    j.pos0 = ((u.first >> 4) + local) * kBlock;
-    const int page = c.table[(long long)u.slot * c.max_pages + (j.pos0 >> c.t_log2)];
-    if (page < 0 || page >= c.n_pages || (STORE && c.refs[page] != 1)) {
-        atomicOr(c.err, kErrBadSegment);
-        return j;
-    }
-    j.page = pages + page * c.page_bytes;
-    j.in_page = j.pos0 & ((1 << c.t_log2) - 1);
-    j.ok = true;
-    return j;
+    const int s = uniform(last_not_above(sp.n_seqs, item, [&](int k) { return (sp.row_starts[k] >> 4) + 2 * k; }));
+    if (s < 0) return false;
+    j.slot = sp.slots ? sp.slots[s] : s;
+    j.row0 = sp.row_starts[s];
+    const int end = sp.row_starts[s + 1];
+    j.first = sp.first[s];
+    j.rows_ok = j.row0 >= 0 && end >= j.row0 && end <= sp.n_rows;
+    j.n = j.rows_ok ? end - j.row0 : 0;
+    const int local = item - ((j.row0 >> 4) + 2 * s);
+    const bool reach = j.first >= 0 && j.n <= c.max_len - j.first;
+    // (a span that cannot be used is reported by the wave of its first item)
+    if (local < 0) return false;                       // (row_starts that decrease)
+    if (local > 0 && (!j.rows_ok || !reach || local > ((j.first + j.n - 1) >> 4) - (j.first >> 4))) return false;
+    if (j.rows_ok && j.n == 0) return false;
+    if (!reach) j.rows_ok = false;
+    j.pos0 = j.rows_ok ? ((j.first >> 4) + local) * kBlock : 0;
+    const int slot = min(max(j.slot, 0), c.n_slots - 1);
+    j.len = c.lens[slot];
+    j.page = c.table[(long long)slot * c.max_pages + (j.pos0 >> c.t_log2)];
+    if (j.slot != slot) j.rows_ok = false;
+    return true;
+}
+__device__ __forceinline__ bool usable(const CacheView& c, const BlockJob& j)
+{
+    return j.rows_ok && j.len >= 0 && j.len <= c.max_len && j.first <= j.len && j.n <= j.len - j.first && j.page >= 0 && j.page < c.n_pages;
 }
 
 template <int N>
-__device__ __forceinline__ void load_bf16(const u16* p, float* f)   // N = 4 or 8 consecutive elements
-{
-    if constexpr (N == 8) unpack8(*reinterpret_cast<const u32x4*>(p), f);
-    else {
-        const u32x2 w = *reinterpret_cast<const u32x2*>(p);
-        f[0] = bf16_lo(w.x); f[1] = bf16_hi(w.x);
-        f[2] = bf16_lo(w.y); f[3] = bf16_hi(w.y);
+struct Packed {                                  // N = 4 or 8 consecutive bf16 elements
+    unsigned int w[N / 2];
+    __device__ __forceinline__ void load(const u16* p)
+    {
+        if constexpr (N == 8) {
+            const u32x4 v = *reinterpret_cast<const u32x4*>(p);
+            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+        } else {
+            const u32x2 v = *reinterpret_cast<const u32x2*>(p);
+            w[0] = v.x; w[1] = v.y;
+        }
     }
-}
+    __device__ __forceinline__ float at(int i) const { return i % 2 ? bf16_hi(w[i / 2]) : bf16_lo(w[i / 2]); }
+};
 
 __device__ __forceinline__ bool finite(float v) { return fabsf(v) < __builtin_inff(); }
 
@@ -128,38 +140,64 @@ __global__ __launch_bounds__(256) void store_rows_kernel(CacheView c, Spans sp, 
     const int wid = uniform((int)blockIdx.x * 4 + (int)threadIdx.x / kWave);
     const int item = wid / c.n_kv_heads, head = wid - item * c.n_kv_heads;
     if (item >= n_items) return;
-    const BlockJob j = find_block<true>(c, sp, pages, item);
-    if (!j.ok) return;
+    BlockJob j;
+    if (!find_block(c, sp, item, j)) return;
     const int lane = lane_id(), kg = lane >> 4, m = lane & 15;
     const int T = 1 << c.t_log2;
-    const bool has_old = j.first > j.pos0;
-    uint8_t* kc = const_cast<uint8_t*>(j.page) + (long long)head * 2 * T * HD + (j.in_page + 4 * kg) * HD + m * D;
-    uint8_t* vc = const_cast<uint8_t*>(j.page) + (long long)(head * 2 + 1) * T * HD + (j.in_page + 4 * kg) * HD + m * D * 4;
-    uint8_t* se = const_cast<uint8_t*>(j.page) + c.scale_off + (head * (T / kBlock) + j.in_page / kBlock) * 2;
     const int pos = j.pos0 + 4 * kg;            // this lane's positions: pos .. pos + 3
 
-    float kv[2][4][D];
-    float amax[2] = {0.f, 0.f};
+    Packed<D> kv[2][4];                         // bf16 pairs
     unsigned int is_new = 0;
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
         const int i = pos + t - j.first;
         const bool live = i >= 0 && i < j.n;
         is_new |= live ? 1u << t : 0u;
-        const long long row = j.row0 + (live ? i : 0);
-        load_bf16<D>(k + row * ldk + head * HD + m * D, kv[0][t]);
-        load_bf16<D>(v + row * ldv + head * HD + m * D, kv[1][t]);
-        if (!live) continue;
+        const long long row = min(max(j.row0 + (live ? i : 0), 0), sp.n_rows - 1);
+        kv[0][t].load(k + row * ldk + head * HD + m * D);
+        kv[1][t].load(v + row * ldv + head * HD + m * D);
+    }
+    if (!usable(c, j)) {
+        if (lane == 0) atomicOr(c.err, kErrBadSegment);
+        return;
+    }
+    const bool has_old = j.first > j.pos0;
+    const int in_page = j.pos0 & (T - 1);
+    uint8_t* page = pages + j.page * c.page_bytes;
+    uint8_t* kc = page + (long long)head * 2 * T * HD + (in_page + 4 * kg) * HD + m * D;
+    uint8_t* vc = page + (long long)(head * 2 + 1) * T * HD + (in_page + 4 * kg) * HD + m * D * 4;
+    uint8_t* se = page + c.scale_off + (head * (T / kBlock) + in_page / kBlock) * 2;
+    const int refs = c.refs[j.page];
+    unsigned int old_k[4][W] = {}, old_v[D] = {};
+    unsigned int old_e = 0;
+    if (has_old) {
+        old_e = *reinterpret_cast<const u16*>(se);
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < W; ++i) old_k[t][i] = reinterpret_cast<const unsigned int*>(kc + t * HD)[i];
+#pragma unroll
+        for (int d = 0; d < D; ++d) old_v[d] = reinterpret_cast<const unsigned int*>(vc)[d];
+    }
+    float amax[2] = {0.f, 0.f};
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
-            for (int d = 0; d < D; ++d) amax[x] = fmaxf(amax[x], finite(kv[x][t][d]) ? fabsf(kv[x][t][d]) : 0.f);
+            for (int d = 0; d < D; ++d) {
+                const float f = kv[x][t].at(d);
+                amax[x] = fmaxf(amax[x], (is_new >> t & 1u) && finite(f) ? fabsf(f) : 0.f);
+            }
+    if (refs != 1) {
+        if (lane == 0) atomicOr(c.err, kErrBadSegment);
+        return;
     }
     int e[2], e_old[2];
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
         e[x] = scale_exponent(wave_max(amax[x]));
-        e_old[x] = has_old ? (int)se[x] - 127 : e[x];
+        e_old[x] = has_old ? (int)(old_e >> (8 * x) & 0xffu) - 127 : e[x];
         e[x] = max(e[x], e_old[x]);
     }
     unsigned int is_old = 0;                    // positions whose codes stay (brought to the new exponent)
@@ -177,10 +215,11 @@ __global__ __launch_bounds__(256) void store_rows_kernel(CacheView c, Spans sp, 
         for (int i = 0; i < W; ++i) {
             float f[4];
             if (again) {
-                decode4(reinterpret_cast<const unsigned int*>(kc + t * HD)[i], block_scale((unsigned)(127 + e_old[0])), f);
+                decode4(old_k[t][i], block_scale((unsigned)(127 + e_old[0])), f);
                 w[i] = encode4(f, rk);
             } else {
-                w[i] = encode4(&kv[0][t][4 * i], rk);
+                const float f4[4] = {kv[0][t].at(4 * i), kv[0][t].at(4 * i + 1), kv[0][t].at(4 * i + 2), kv[0][t].at(4 * i + 3)};
+                w[i] = encode4(f4, rk);
             }
         }
 #pragma unroll
@@ -192,16 +231,13 @@ __global__ __launch_bounds__(256) void store_rows_kernel(CacheView c, Spans sp, 
     if (is_new || again) {
 #pragma unroll
         for (int d = 0; d < D; ++d) {
-            unsigned int old = 0;
-            if (is_new != 15u) {
-                old = reinterpret_cast<const unsigned int*>(vc)[d];
-                if (again) {
-                    float f[4];
-                    decode4(old, block_scale((unsigned)(127 + e_old[1])), f);
-                    old = encode4(f, rv);
-                }
+            unsigned int old = old_v[d];        // (positions behind the last row: nobody's)
+            if (again) {
+                float f[4];
+                decode4(old, block_scale((unsigned)(127 + e_old[1])), f);
+                old = encode4(f, rv);
             }
-            const float f[4] = {kv[1][0][d], kv[1][1][d], kv[1][2][d], kv[1][3][d]};
+            const float f[4] = {kv[1][0].at(d), kv[1][1].at(d), kv[1][2].at(d), kv[1][3].at(d)};
             reinterpret_cast<unsigned int*>(vc)[d] = (encode4(f, rv) & sel) | (old & ~sel);
         }
     }
@@ -216,13 +252,24 @@ __global__ __launch_bounds__(256) void load_rows_kernel(CacheView c, Spans sp, c
     const int wid = uniform((int)blockIdx.x * 4 + (int)threadIdx.x / kWave);
     const int item = wid / c.n_kv_heads, head = wid - item * c.n_kv_heads;
     if (item >= n_items) return;
-    const BlockJob j = find_block<false>(c, sp, pages, item);
-    if (!j.ok) return;
+    BlockJob j;
+    if (!find_block(c, sp, item, j)) return;
     const int lane = lane_id(), kg = lane >> 4, m = lane & 15;
     const int T = 1 << c.t_log2;
-    const uint8_t* kc = j.page + (long long)head * 2 * T * HD + (j.in_page + 4 * kg) * HD + m * D;
-    const uint8_t* vc = j.page + (long long)(head * 2 + 1) * T * HD + (j.in_page + 4 * kg) * HD + m * D * 4;
-    const uint8_t* se = j.page + c.scale_off + (head * (T / kBlock) + j.in_page / kBlock) * 2;
+    if (!usable(c, j)) {
+        if (lane == 0) atomicOr(c.err, kErrBadSegment);
+        return;
+    }
+    const int in_page = j.pos0 & (T - 1);
+    const uint8_t* page = pages + j.page * c.page_bytes;
+    const uint8_t* kc = page + (long long)head * 2 * T * HD + (in_page + 4 * kg) * HD + m * D;
+    const uint8_t* vc = page + (long long)(head * 2 + 1) * T * HD + (in_page + 4 * kg) * HD + m * D * 4;
+    const uint8_t* se = page + c.scale_off + (head * (T / kBlock) + in_page / kBlock) * 2;
+    unsigned int kw[4][W];
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int w = 0; w < W; ++w) kw[t][w] = reinterpret_cast<const unsigned int*>(kc + t * HD)[w];
     const float sk = block_scale(se[0]), sv = block_scale(se[1]);
     unsigned int vw[D];
 #pragma unroll
@@ -240,7 +287,7 @@ __global__ __launch_bounds__(256) void load_rows_kernel(CacheView c, Spans sp, c
 #pragma unroll
         for (int w = 0; w < W; ++w) {
             float f[4];
-            decode4(reinterpret_cast<const unsigned int*>(kc + t * HD)[w], sk, f);
+            decode4(kw[t][w], sk, f);
             reinterpret_cast<u32x2*>(ko)[w] = u32x2{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3])};
             reinterpret_cast<u32x2*>(vo)[w] = u32x2{pack_bf16x2(vf[4 * w][t], vf[4 * w + 1][t]), pack_bf16x2(vf[4 * w + 2][t], vf[4 * w + 3][t])};
         }
@@ -249,12 +296,16 @@ __global__ __launch_bounds__(256) void load_rows_kernel(CacheView c, Spans sp, c
 
 // =================================================================================================
 // Page management.  The state is three integer arrays; every call is a function of them that does not depend on the order in
-// which workgroups run.  Pages are counted in segments of 4096; the plan of the requests (which slot, how many pages, running
-// sum) is made by one workgroup while others count the free pages, and the next launch hands the lowest free
-// pages out: every segment's workgroup adds up the counts before it, and finds the request of a free page by its rank.
+// which workgroups run.  First the plan: which request gets how many pages (a running sum), and which pages are free (a rank).
+// Up to kSmallPages pages one workgroup does all of it in one launch; beyond, pages are counted in segments by a workgroup each beside
+// the requests' plan, and a second launch hands out.  What the plan leaves (table rows, copies of pages) is the last launch's.
 // =================================================================================================
 constexpr int kSegPages = 4096;
-constexpr int kPlanThreads = 256;
+constexpr int kSmallPages = 8192;       // pages up to which one workgroup does it (1024 a round)
+constexpr int kRefGroups = 16;          // workgroups that move the counts of a compaction's pages
+constexpr int kMarkSlots = 8192;        // slots whose first mention is looked for in LDS; of more, in the workspace
+constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / kWave;
+constexpr int kSegThreads = 256;
 
 // The workspace behind its header.
 struct PagePlan {
@@ -273,9 +324,11 @@ struct PagePlan {
     int* totals;        // [4]
 };
 
+int segments_of(int n_pages) { return (n_pages + kSegPages - 1) / kSegPages; }
+
 size_t plan_ints(int n_pages, int n_slots, int n)
 {
-    return (size_t)(n_pages + kSegPages - 1) / kSegPages + 7 * (size_t)n + (size_t)n_slots + 3 * (size_t)n_pages + 4;
+    return (size_t)segments_of(n_pages) + 7 * (size_t)n + (size_t)n_slots + 3 * (size_t)n_pages + 4;
 }
 
 PagePlan plan_of(void* workspace, int n_pages, int n_slots, int n)
@@ -283,7 +336,7 @@ PagePlan plan_of(void* workspace, int n_pages, int n_slots, int n)
     PagePlan p;
     int* at = reinterpret_cast<int*>(static_cast<char*>(workspace) + kWsHeaderBytes);
     const auto take = [&](size_t k) { int* q = at; at += k; return q; };
-    p.seg_free = take((size_t)(n_pages + kSegPages - 1) / kSegPages);
+    p.seg_free = take(segments_of(n_pages));
     p.slot = take(n); p.have = take(n); p.add = take(n); p.src = take(n); p.upto = take(n); p.page = take(n); p.from = take(n);
     p.mark = take(n_slots);
     p.list_src = take(n_pages); p.list_dst = take(n_pages); p.rank = take(n_pages);
@@ -291,13 +344,10 @@ PagePlan plan_of(void* workspace, int n_pages, int n_slots, int n)
     return p;
 }
 
-__device__ __forceinline__ int wave_sum(int v)
-{
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) v += __shfl_xor(v, d, kWave);
-    return v;
-}
-// sum over the workgroup of kPlanThreads threads (slot: kPlanThreads / 64 ints of LDS)
+__device__ __forceinline__ int wave_sum(int v) { return lane_value(wave_inclusive_scan(v), kWave - 1); }
+
+// sum over a workgroup of WAVES waves, in every thread (slot: WAVES ints of LDS)
+template <int WAVES>
 __device__ __forceinline__ int block_sum(int v, int* slot)
 {
     v = wave_sum(v);
@@ -306,10 +356,11 @@ __device__ __forceinline__ int block_sum(int v, int* slot)
     __syncthreads();
     int s = 0;
 #pragma unroll
-    for (int w = 0; w < kPlanThreads / kWave; ++w) s += slot[w];
+    for (int w = 0; w < WAVES; ++w) s += slot[w];
     return s;
 }
 // inclusive prefix sum over the workgroup; total: the whole sum
+template <int WAVES>
 __device__ __forceinline__ int block_scan(int v, int* slot, int* total)
 {
     const int inc = wave_inclusive_scan(v);
@@ -318,7 +369,7 @@ __device__ __forceinline__ int block_scan(int v, int* slot, int* total)
     __syncthreads();
     int before = 0, all = 0;
 #pragma unroll
-    for (int w = 0; w < kPlanThreads / kWave; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
         if (w < (int)threadIdx.x / kWave) before += slot[w];
         all += slot[w];
     }
@@ -326,37 +377,41 @@ __device__ __forceinline__ int block_scan(int v, int* slot, int* total)
     return inc + before;
 }
 
-// pages of segment seg with refs > 0 (LIVE) or refs <= 0, counted by the workgroup
-template <bool LIVE>
-__device__ __forceinline__ void count_segment(const CacheView& c, int seg, int* seg_count, int* slot)
+// first request whose running sum is above r, of n
+__device__ __forceinline__ int request_of(const int* upto, int n, int r)
 {
-    int n = 0;
-    for (int i = (int)threadIdx.x; i < kSegPages; i += kPlanThreads) {
-        const int p = seg * kSegPages + i;
-        if (p < c.n_pages) n += (c.refs[p] > 0) == LIVE;
+    int lo = 0, hi = n;
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (upto[mid] > r) hi = mid;
+        else lo = mid + 1;
     }
-    n = block_sum(n, slot);
-    if (threadIdx.x == 0) seg_count[seg] = n;
+    return lo;
 }
 
 struct Requests { const int32_t* slots; const int32_t* dst; const int32_t* amount; int n; };  // dst: fork; amount: add or keep
 
-// Launch 1: workgroup 0 plans the requests, the others count.
+// The requests' plan, by one workgroup of kPlanThreads.
 template <bool FORK>
-__global__ __launch_bounds__(kPlanThreads) void plan_kernel(CacheView c, PagePlan p, Requests rq)
+__device__ void plan_requests(const CacheView& c, const PagePlan& p, const Requests& rq, int* marks, int* sums)
 {
-    __shared__ int slot_sums[kPlanThreads / kWave];
-    if (blockIdx.x > 0) {
-        count_segment<false>(c, (int)blockIdx.x - 1, p.seg_free, slot_sums);
-        return;
-    }
     const int32_t* changed = FORK ? rq.dst : rq.slots;     // slots that the call writes
     const auto in_range = [&](int s) { return s >= 0 && s < c.n_slots; };
-    for (int i = (int)threadIdx.x; i < rq.n; i += kPlanThreads)
-        if (in_range(changed[i])) __hip_atomic_store(p.mark + changed[i], 0x7fffffff, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    // the first request that lists a slot is the one that counts
+    const bool in_lds = c.n_slots <= kMarkSlots;
+    for (int i = (int)threadIdx.x; i < rq.n; i += kPlanThreads) {
+        const int s = changed[i];
+        if (!in_range(s)) continue;
+        if (in_lds) marks[s] = 0x7fffffff;
+        else __hip_atomic_store(p.mark + s, 0x7fffffff, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
     __syncthreads();
-    for (int i = (int)threadIdx.x; i < rq.n; i += kPlanThreads)
-        if (in_range(changed[i])) __hip_atomic_fetch_min(p.mark + changed[i], i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    for (int i = (int)threadIdx.x; i < rq.n; i += kPlanThreads) {
+        const int s = changed[i];
+        if (!in_range(s)) continue;
+        if (in_lds) atomicMin(marks + s, i);
+        else __hip_atomic_fetch_min(p.mark + s, i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
     __syncthreads();
     const int T = 1 << c.t_log2;
     int base = 0;
@@ -364,16 +419,17 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(CacheView c, PagePla
         const int i = i0 + (int)threadIdx.x;
         int need = 0;
         if (i < rq.n) {
-            const int s = changed[i];
-            bool ok = in_range(s) && __hip_atomic_load(p.mark + s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == i;
-            const int len = ok ? c.lens[s] : 0;
+            const int s = changed[i], slot = min(max(s, 0), c.n_slots - 1);
+            const int len = c.lens[slot];
+            const int first = in_lds ? marks[slot] : __hip_atomic_load(p.mark + slot, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            bool ok = in_range(s) && first == i;
             int have = 0, add = 0, from = -1, src = -1;
             if (FORK) {
                 src = rq.slots[i];
-                ok = ok && in_range(src) && len == 0;
-                const int all = ok ? c.lens[src] : 0;
+                const int parent = min(max(src, 0), c.n_slots - 1);
+                const int all = c.lens[parent];
                 add = rq.amount ? rq.amount[i] : all;
-                ok = ok && all <= c.max_len && add >= 0 && add <= all;
+                ok = ok && in_range(src) && len == 0 && all <= c.max_len && add >= 0 && add <= all;
                 if (ok) {
                     have = add >> c.t_log2;
                     need = (add & (T - 1)) != 0;
@@ -405,114 +461,237 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(CacheView c, PagePla
             }
         }
         int total;
-        const int inc = block_scan(need, slot_sums, &total);
+        const int inc = block_scan<kPlanWaves>(need, sums, &total);
         if (i < rq.n) p.upto[i] = min(base + inc, c.n_pages + 1);
         base = min(base + total, c.n_pages + 1);
         __syncthreads();
     }
 }
 
-// first request whose running sum is above r, of n
-__device__ __forceinline__ int request_of(const int* upto, int n, int r)
+// Hands free page `page` of rank r (counted among the free pages) to its request; all: free pages there are.
+template <bool FORK>
+__device__ __forceinline__ void hand_out(const CacheView& c, const PagePlan& p, const int* upto, int n, int page, int r, int all)
 {
-    int lo = 0, hi = n;
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (upto[mid] > r) hi = mid;
-        else lo = mid + 1;
-    }
-    return lo;
+    const int i = request_of(upto, n, r);
+    if (upto[i] > all) return;                   // this request is not served
+    const int mine = r - (i ? upto[i - 1] : 0);
+    c.table[(long long)p.slot[i] * c.max_pages + p.have[i] + mine] = page;
+    c.refs[page] = 1;
+    if (FORK) p.page[i] = page;
 }
 
-// Launch 2: workgroup g < segments hands out the free pages of segment g; the others (fork: one request each wave; reserve: lengths)
-// bring the slots' state up to date.
+// Requests that the free pages do not reach are taken out of the plan and reported; lengths of the others (reserve).
+template <bool FORK>
+__device__ __forceinline__ void settle(const CacheView& c, const PagePlan& p, const int* upto, int i, int all)
+{
+    if (upto[i] > all) {
+        atomicOr(c.err, kErrNoPages);
+        p.slot[i] = -1;
+    } else if (!FORK && p.slot[i] >= 0) c.lens[p.slot[i]] += p.add[i];
+}
+
+// Running sums of the requests in LDS, where they are looked up (of more than kMarkSlots requests: in the workspace).
+template <int THREADS>
+__device__ __forceinline__ const int* keep_sums(const PagePlan& p, int n, int* lds)
+{
+    if (n > kMarkSlots) return p.upto;
+    for (int i = (int)threadIdx.x; i < n; i += THREADS) lds[i] = p.upto[i];
+    return lds;
+}
+
+// Up to kSmallPages pages: plan and hand-out by one workgroup.
+template <bool FORK>
+__global__ __launch_bounds__(kPlanThreads) void plan_small_kernel(CacheView c, PagePlan p, Requests rq)
+{
+    constexpr int ROUNDS = kSmallPages / kPlanThreads;
+    __shared__ int marks[kMarkSlots];
+    __shared__ int sums[kPlanWaves];
+    // whether page r * 1024 + thread is free: bit r
+    unsigned int is_free = 0;
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+        const int page = r * kPlanThreads + (int)threadIdx.x;
+        is_free |= c.refs[min(page, c.n_pages - 1)] <= 0 && page < c.n_pages ? 1u << r : 0u;
+    }
+    plan_requests<FORK>(c, p, rq, marks, sums);
+    const int* upto = keep_sums<kPlanThreads>(p, rq.n, marks);
+    const int all = block_sum<kPlanWaves>(__popc(is_free), sums);       // (its barriers: the sums are there)
+    const int wanted = upto[rq.n - 1];
+    int before = 0;
+    for (int r = 0; r * kPlanThreads < c.n_pages && before < wanted; ++r) {
+        const bool mine = is_free >> r & 1u;
+        int total;
+        const int rank = before + block_scan<kPlanWaves>(mine ? 1 : 0, sums, &total) - 1;
+        if (mine && rank < wanted) hand_out<FORK>(c, p, upto, rq.n, r * kPlanThreads + (int)threadIdx.x, rank, all);
+        before += total;
+    }
+    for (int i = (int)threadIdx.x; i < rq.n; i += kPlanThreads) settle<FORK>(c, p, upto, i, all);
+}
+
+// Beyond kSmallPages, first launch: workgroup 0 plans, the others count the free pages of a segment each.
+template <bool LIVE, int THREADS>
+__device__ __forceinline__ void count_segment(const CacheView& c, int seg, int* seg_count, int* sums)
+{
+    int n = 0;
+    for (int i = (int)threadIdx.x; i < kSegPages; i += THREADS) {
+        const int p = seg * kSegPages + i;
+        if (p < c.n_pages) n += (c.refs[p] > 0) == LIVE;
+    }
+    n = block_sum<THREADS / kWave>(n, sums);
+    if (threadIdx.x == 0) seg_count[seg] = n;
+}
+
+template <bool FORK>
+__global__ __launch_bounds__(kPlanThreads) void plan_kernel(CacheView c, PagePlan p, Requests rq)
+{
+    __shared__ int marks[kMarkSlots];
+    __shared__ int sums[kPlanWaves];
+    if (blockIdx.x > 0) count_segment<false, kPlanThreads>(c, (int)blockIdx.x - 1, p.seg_free, sums);
+    else plan_requests<FORK>(c, p, rq, marks, sums);
+}
+
+// Second launch: workgroup g < segments hands out the free pages of segment g, the last one settles the requests.
 template <bool FORK>
 __global__ __launch_bounds__(kPlanThreads) void assign_kernel(CacheView c, PagePlan p, int n, int n_seg)
 {
-    __shared__ int sums[kPlanThreads / kWave];
+    constexpr int WAVES = kPlanWaves, ROUNDS = kSegPages / kPlanThreads;
+    __shared__ int lds[kMarkSlots];
+    __shared__ int sums[WAVES];
     int before = 0, all = 0;
     const int seg = (int)blockIdx.x;
+    unsigned int is_free = 0;                   // whether page r * 1024 + thread of the segment is free: bit r
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+        const int page = seg * kSegPages + r * kPlanThreads + (int)threadIdx.x;
+        is_free |= c.refs[min(page, c.n_pages - 1)] <= 0 && page < c.n_pages ? 1u << r : 0u;
+    }
     for (int s = (int)threadIdx.x; s < n_seg; s += kPlanThreads) {
         const int f = p.seg_free[s];
         all += f;
         before += s < seg ? f : 0;
     }
-    all = block_sum(all, sums);
-    before = block_sum(before, sums);
-    const int wanted = p.upto[n - 1];
-    if (seg < n_seg) {
-        if (before >= wanted) return;
-        for (int i0 = 0; i0 < kSegPages; i0 += kPlanThreads) {
-            const int page = seg * kSegPages + i0 + (int)threadIdx.x;
-            const bool is_free = page < c.n_pages && c.refs[page] <= 0;
-            int total;
-            const int r = before + block_scan(is_free ? 1 : 0, sums, &total) - 1;
-            if (is_free && r < wanted) {
-                const int i = request_of(p.upto, n, r);
-                if (p.upto[i] <= all) {
-                    const int mine = r - (i ? p.upto[i - 1] : 0);
-                    c.table[(long long)p.slot[i] * c.max_pages + p.have[i] + mine] = page;
-                    c.refs[page] = 1;
-                    if (FORK) p.page[i] = page;
-                }
-            }
-            before += total;
-            if (before >= wanted) break;
-        }
+    const int* upto = keep_sums<kPlanThreads>(p, n, lds);
+    all = block_sum<WAVES>(all, sums);
+    before = block_sum<WAVES>(before, sums);
+    if (seg == n_seg) {
+        for (int i = (int)threadIdx.x; i < n; i += kPlanThreads) settle<FORK>(c, p, upto, i, all);
         return;
     }
-    if (!FORK) {
-        for (int i = (seg - n_seg) * kPlanThreads + (int)threadIdx.x; i < n; i += kPlanThreads * ((int)gridDim.x - n_seg)) {
-            if (p.upto[i] > all) atomicOr(c.err, kErrNoPages);
-            else if (p.slot[i] >= 0) c.lens[p.slot[i]] += p.add[i];
-        }
-        return;
+    const int wanted = upto[n - 1];
+    for (int r = 0; r < ROUNDS && before < wanted; ++r) {
+        const bool mine = is_free >> r & 1u;
+        int total;
+        const int rank = before + block_scan<WAVES>(mine ? 1 : 0, sums, &total) - 1;
+        if (mine && rank < wanted) hand_out<FORK>(c, p, upto, n, seg * kSegPages + r * kPlanThreads + (int)threadIdx.x, rank, all);
+        before += total;
     }
-    const int i = (seg - n_seg) * (kPlanThreads / kWave) + (int)threadIdx.x / kWave;
-    if (i >= n) return;
-    if (p.upto[i] > all) {
-        if (lane_id() == 0) atomicOr(c.err, kErrNoPages);
-        return;
-    }
-    const int dst = p.slot[i];
-    if (dst < 0) return;
-    const int32_t* from = c.table + (long long)p.src[i] * c.max_pages;
-    int32_t* to = c.table + (long long)dst * c.max_pages;
-    for (int j = lane_id(); j < p.have[i]; j += kWave) {
-        const int page = from[j];
-        to[j] = page;
-        if (page >= 0 && page < c.n_pages) atomicAdd(c.refs + page, 1);
-        else atomicOr(c.err, kErrBadSegment);
-    }
-    if (lane_id() == 0) c.lens[dst] = p.add[i];
 }
 
-// ---- whole pages, in every pool: 16 KB a step of a workgroup --------------------------------------------------------
+// ---- compact: lists of the pages that move and of where they go, and every page's place in the list (-1: stays) --------
+// pages in use up to `page`, itself included: upto; among the first n_live pages: low
+__device__ __forceinline__ void list_page(const CacheView& c, const PagePlan& p, int page, bool live, int upto, int n_live, int low)
+{
+    if (page >= c.n_pages) return;
+    int rank = -1;
+    if (live && page >= n_live) {
+        rank = upto - 1 - low;
+        p.list_src[rank] = page;
+    }
+    if (!live && page < n_live) p.list_dst[page - upto] = page;
+    p.rank[page] = rank;
+}
+
+__global__ __launch_bounds__(kPlanThreads) void list_small_kernel(CacheView c, PagePlan p)
+{
+    __shared__ int sums[kPlanWaves];
+    int n = 0;
+#pragma unroll 8
+    for (int i = (int)threadIdx.x; i < c.n_pages; i += kPlanThreads) n += c.refs[i] > 0;
+    const int n_live = block_sum<kPlanWaves>(n, sums);
+    n = 0;
+#pragma unroll 8
+    for (int i = (int)threadIdx.x; i < n_live; i += kPlanThreads) n += c.refs[i] > 0;
+    const int low = block_sum<kPlanWaves>(n, sums);
+    if (threadIdx.x == 0) {
+        p.totals[0] = n_live - low;
+        p.totals[1] = n_live;
+    }
+    int before = 0;
+    for (int p0 = 0; p0 < c.n_pages; p0 += kPlanThreads) {
+        const int page = p0 + (int)threadIdx.x;
+        const bool live = page < c.n_pages && c.refs[page] > 0;
+        int total;
+        const int upto = before + block_scan<kPlanWaves>(live ? 1 : 0, sums, &total);
+        list_page(c, p, page, live, upto, n_live, low);
+        before += total;
+    }
+}
+
+__global__ __launch_bounds__(kSegThreads) void count_live_kernel(CacheView c, PagePlan p)
+{
+    __shared__ int sums[kSegThreads / kWave];
+    count_segment<true, kSegThreads>(c, (int)blockIdx.x, p.seg_free, sums);
+}
+
+__global__ __launch_bounds__(kSegThreads) void list_moves_kernel(CacheView c, PagePlan p, int n_seg)
+{
+    constexpr int WAVES = kSegThreads / kWave;
+    __shared__ int sums[WAVES];
+    const int seg = (int)blockIdx.x;
+    int before = 0, n_live = 0;
+    for (int s = (int)threadIdx.x; s < n_seg; s += kSegThreads) {
+        const int f = p.seg_free[s];
+        n_live += f;
+        before += s < seg ? f : 0;
+    }
+    n_live = block_sum<WAVES>(n_live, sums);
+    before = block_sum<WAVES>(before, sums);
+    // pages in use among the first n_live: whole segments by their counts, the one that n_live cuts by its refs
+    const int cut = n_live / kSegPages;
+    int low = 0;
+    for (int s = (int)threadIdx.x; s < min(cut, n_seg); s += kSegThreads) low += p.seg_free[s];
+    for (int i = cut * kSegPages + (int)threadIdx.x; i < n_live; i += kSegThreads) low += c.refs[i] > 0;
+    low = block_sum<WAVES>(low, sums);
+    if (seg == 0 && threadIdx.x == 0) {
+        p.totals[0] = n_live - low;
+        p.totals[1] = n_live;
+    }
+    for (int i0 = 0; i0 < kSegPages; i0 += kSegThreads) {
+        const int page = seg * kSegPages + i0 + (int)threadIdx.x;
+        const bool live = page < c.n_pages && c.refs[page] > 0;
+        int total;
+        const int upto = before + block_scan<WAVES>(live ? 1 : 0, sums, &total);
+        list_page(c, p, page, live, upto, n_live, low);
+        before += total;
+    }
+}
+
+// ---- last launch of a fork or a compaction: state that follows the plan by the first workgroups, whole pages (in every pool, 16 KB
+// a step) by the others --------------------------------------------------------------------------------------------------
 constexpr int kCopyThreads = 256, kCopyBytes = 16384;
 
 __device__ __forceinline__ void copy_piece(const uint8_t* src, uint8_t* dst, int bytes)   // a multiple of 16, at most kCopyBytes
 {
-    u32x4 v[kCopyBytes / (16 * kCopyThreads)];
     constexpr int N = kCopyBytes / (16 * kCopyThreads);
+    u32x4 v[N];
 #pragma unroll
     for (int k = 0; k < N; ++k) {
         const int at = (k * kCopyThreads + (int)threadIdx.x) * 16;
-        if (at < bytes) v[k] = *reinterpret_cast<const u32x4*>(src + at);
+        if (at < bytes) v[k] = load_once<true>(src + at);
     }
 #pragma unroll
     for (int k = 0; k < N; ++k) {
         const int at = (k * kCopyThreads + (int)threadIdx.x) * 16;
-        if (at < bytes) *reinterpret_cast<u32x4*>(dst + at) = v[k];
+        if (at < bytes) store_once<true>(dst + at, v[k]);
     }
 }
 
-__global__ __launch_bounds__(kCopyThreads) void copy_pages_kernel(CacheView c, const int* src, const int* dst, const int* n_dev, int n_host,
-                                                                  void* const* pools, int n_pools)
+// first: workgroup among the copying ones
+__device__ __forceinline__ void copy_pages(const CacheView& c, const int* src, const int* dst, int n, void* const* pools, int n_pools, int first, int groups)
 {
-    const int n = n_dev ? *n_dev : n_host;
     const int pieces = (int)((c.page_bytes + kCopyBytes - 1) / kCopyBytes);
     const long long units = (long long)n * n_pools * pieces;
-    for (long long u = blockIdx.x; u < units; u += gridDim.x) {
+    for (long long u = first; u < units; u += groups) {
         const int piece = (int)(u % pieces);
         const int i = (int)(u / pieces % n), pool = (int)(u / pieces / n);
         const int from = src[i], to = dst[i];
@@ -523,7 +702,63 @@ __global__ __launch_bounds__(kCopyThreads) void copy_pages_kernel(CacheView c, c
     }
 }
 
-__global__ __launch_bounds__(kPlanThreads) void free_kernel(CacheView c, const int32_t* slots)
+// n_state workgroups take the children's table rows, a wave each
+__global__ __launch_bounds__(kCopyThreads) void fork_kernel(CacheView c, PagePlan p, int n, int n_state, void* const* pools, int n_pools)
+{
+    if ((int)blockIdx.x >= n_state) {
+        copy_pages(c, p.from, p.page, n, pools, n_pools, (int)blockIdx.x - n_state, (int)gridDim.x - n_state);
+        return;
+    }
+    const int i = (int)blockIdx.x * (kCopyThreads / kWave) + (int)threadIdx.x / kWave;
+    if (i >= n || p.slot[i] < 0) return;
+    const int32_t* from = c.table + (long long)p.src[i] * c.max_pages;
+    int32_t* to = c.table + (long long)p.slot[i] * c.max_pages;
+    for (int j = lane_id(); j < p.have[i]; j += kWave) {
+        const int page = from[j];
+        to[j] = page;
+        if (page >= 0 && page < c.n_pages) atomicAdd(c.refs + page, 1);
+        else atomicOr(c.err, kErrBadSegment);
+    }
+    if (lane_id() == 0) c.lens[p.slot[i]] = p.add[i];
+}
+
+// the first kRefGroups workgroups move the refs, the next n_slots take a slot's table row each
+__global__ __launch_bounds__(kCopyThreads) void compact_kernel(CacheView c, PagePlan p, int32_t* n_live, void* const* pools, int n_pools)
+{
+    const int moves = p.totals[0], n_state = kRefGroups + c.n_slots;
+    if ((int)blockIdx.x >= n_state) {
+        if (moves > 0) copy_pages(c, p.list_src, p.list_dst, moves, pools, n_pools, (int)blockIdx.x - n_state, (int)gridDim.x - n_state);
+        return;
+    }
+    if ((int)blockIdx.x < kRefGroups) {
+        for (int i = (int)blockIdx.x * kCopyThreads + (int)threadIdx.x; i < moves; i += kRefGroups * kCopyThreads) {
+            const int from = p.list_src[i], to = p.list_dst[i];
+            c.refs[to] = c.refs[from];
+            c.refs[from] = 0;
+        }
+        if (n_live && blockIdx.x == 0 && threadIdx.x == 0) *n_live = p.totals[1];
+        return;
+    }
+    const int s = (int)blockIdx.x - kRefGroups;
+    const int len = c.lens[s];
+    if (len < 0 || len > c.max_len) {
+        if (threadIdx.x == 0) atomicOr(c.err, kErrBadSegment);
+        return;
+    }
+    const int held = (len + (1 << c.t_log2) - 1) >> c.t_log2;
+    int32_t* row = c.table + (long long)s * c.max_pages;
+    for (int j = (int)threadIdx.x; j < held; j += kCopyThreads) {
+        const int page = row[j];
+        if (page < 0 || page >= c.n_pages) {
+            atomicOr(c.err, kErrBadSegment);
+            continue;
+        }
+        const int r = p.rank[page];
+        if (r >= 0) row[j] = p.list_dst[r];
+    }
+}
+
+__global__ __launch_bounds__(kSegThreads) void free_kernel(CacheView c, const int32_t* slots)
 {
     __shared__ int s_len;
     const int s = slots[blockIdx.x];
@@ -541,7 +776,7 @@ __global__ __launch_bounds__(kPlanThreads) void free_kernel(CacheView c, const i
     }
     const int held = (len + (1 << c.t_log2) - 1) >> c.t_log2;
     int32_t* row = c.table + (long long)s * c.max_pages;
-    for (int j = (int)threadIdx.x; j < held; j += kPlanThreads) {
+    for (int j = (int)threadIdx.x; j < held; j += kSegThreads) {
         const int page = row[j];
         row[j] = -1;
         const bool ok = page >= 0 && page < c.n_pages;
@@ -550,86 +785,6 @@ __global__ __launch_bounds__(kPlanThreads) void free_kernel(CacheView c, const i
         atomicOr(c.err, kErrBadSegment);
     }
 }
-
-// ---- compact --------------------------------------------------------------------------------------------------------
-__global__ __launch_bounds__(kPlanThreads) void count_live_kernel(CacheView c, PagePlan p)
-{
-    __shared__ int sums[kPlanThreads / kWave];
-    count_segment<true>(c, (int)blockIdx.x, p.seg_free, sums);
-}
-
-// Lists of the pages that move and of where they go, and every page's place in the list (-1: stays).
-__global__ __launch_bounds__(kPlanThreads) void list_moves_kernel(CacheView c, PagePlan p, int n_seg)
-{
-    __shared__ int sums[kPlanThreads / kWave];
-    const int seg = (int)blockIdx.x;
-    int before = 0, n_live = 0;
-    for (int s = (int)threadIdx.x; s < n_seg; s += kPlanThreads) {
-        const int f = p.seg_free[s];
-        n_live += f;
-        before += s < seg ? f : 0;
-    }
-    n_live = block_sum(n_live, sums);
-    before = block_sum(before, sums);
-    // pages in use among the first n_live: whole segments by their counts, the one that n_live cuts by its refs
-    const int cut = n_live / kSegPages;
-    int low = 0;
-    for (int s = (int)threadIdx.x; s < min(cut, n_seg); s += kPlanThreads) low += p.seg_free[s];
-    for (int i = cut * kSegPages + (int)threadIdx.x; i < n_live; i += kPlanThreads) low += c.refs[i] > 0;
-    low = block_sum(low, sums);
-    if (seg == 0 && threadIdx.x == 0) {
-        p.totals[0] = n_live - low;
-        p.totals[1] = n_live;
-    }
-    for (int i0 = 0; i0 < kSegPages; i0 += kPlanThreads) {
-        const int page = seg * kSegPages + i0 + (int)threadIdx.x;
-        const bool live = page < c.n_pages && c.refs[page] > 0;
-        int total;
-        const int upto = before + block_scan(live ? 1 : 0, sums, &total);   // pages in use up to this one
-        int rank = -1;
-        if (live && page >= n_live) {
-            rank = upto - 1 - low;
-            p.list_src[rank] = page;
-        }
-        if (!live && page < n_live) p.list_dst[page - upto] = page;
-        if (page < c.n_pages) p.rank[page] = rank;
-        before += total;
-    }
-}
-
-// The first workgroups move the refs, the others rewrite a slot's table row each.
-__global__ __launch_bounds__(kPlanThreads) void follow_moves_kernel(CacheView c, PagePlan p, int n_ref_groups, int32_t* n_live)
-{
-    const int moves = p.totals[0];
-    if ((int)blockIdx.x < n_ref_groups) {
-        for (int i = (int)blockIdx.x * kPlanThreads + (int)threadIdx.x; i < moves; i += n_ref_groups * kPlanThreads) {
-            const int from = p.list_src[i], to = p.list_dst[i];
-            c.refs[to] = c.refs[from];
-            c.refs[from] = 0;
-        }
-        if (n_live && blockIdx.x == 0 && threadIdx.x == 0) *n_live = p.totals[1];
-        return;
-    }
-    const int s = (int)blockIdx.x - n_ref_groups;
-    const int len = c.lens[s];
-    if (len < 0 || len > c.max_len) {
-        if (threadIdx.x == 0) atomicOr(c.err, kErrBadSegment);
-        return;
-    }
-    const int held = (len + (1 << c.t_log2) - 1) >> c.t_log2;
-    int32_t* row = c.table + (long long)s * c.max_pages;
-    for (int j = (int)threadIdx.x; j < held; j += kPlanThreads) {
-        const int page = row[j];
-        if (page < 0 || page >= c.n_pages) {
-            atomicOr(c.err, kErrBadSegment);
-            continue;
-        }
-        const int r = p.rank[page];
-        if (r >= 0) row[j] = p.list_dst[r];
-    }
-}
-
-int segments_of(int n_pages) { return (n_pages + kSegPages - 1) / kSegPages; }
 
 lq_status launched() { return hipGetLastError() == hipSuccess ? LQ_OK : LQ_ERR_HIP; }
 
@@ -643,9 +798,24 @@ lq_status page_call(const lq_cache* c, int32_t n, void* workspace, size_t worksp
     return LQ_OK;
 }
 
-int copy_grid(long long most)
+// copying workgroups for at most `pages` pages of every pool
+int copy_groups(const CacheView& c, long long pages, int n_pools)
 {
-    return (int)(most < 1 ? 1 : most < 4096 ? most : 4096);
+    const long long units = pages * n_pools * ((c.page_bytes + kCopyBytes - 1) / kCopyBytes);
+    return (int)(units < 4096 ? units : 4096);
+}
+
+// plan and hand-out; n > 0
+template <bool FORK>
+void plan_and_assign(const CacheView& c, const PagePlan& p, const Requests& rq, hipStream_t hs)
+{
+    if (c.n_pages <= kSmallPages) {
+        hipLaunchKernelGGL(plan_small_kernel<FORK>, dim3(1), dim3(kPlanThreads), 0, hs, c, p, rq);
+        return;
+    }
+    const int n_seg = segments_of(c.n_pages);
+    hipLaunchKernelGGL(plan_kernel<FORK>, dim3(1 + n_seg), dim3(kPlanThreads), 0, hs, c, p, rq);
+    hipLaunchKernelGGL(assign_kernel<FORK>, dim3(n_seg + 1), dim3(kPlanThreads), 0, hs, c, p, rq.n, n_seg);
 }
 
 template <bool STORE>
@@ -706,11 +876,7 @@ extern "C" lq_status lora_cache_reserve(const lq_cache* host_cache, const int32_
     if (n_seqs > 0 && (!slots || !add)) return LQ_ERR_INVALID_ARG;
     const lq_status st = page_call(host_cache, n_seqs, workspace, workspace_bytes, &c);
     if (st != LQ_OK || n_seqs == 0) return st;
-    const PagePlan p = plan_of(workspace, c.n_pages, c.n_slots, n_seqs);
-    const int n_seg = segments_of(c.n_pages);
-    const hipStream_t hs = static_cast<hipStream_t>(stream);
-    hipLaunchKernelGGL(plan_kernel<false>, dim3(1 + n_seg), dim3(kPlanThreads), 0, hs, c, p, Requests{slots, nullptr, add, n_seqs});
-    hipLaunchKernelGGL(assign_kernel<false>, dim3(n_seg + 1), dim3(kPlanThreads), 0, hs, c, p, n_seqs, n_seg);
+    plan_and_assign<false>(c, plan_of(workspace, c.n_pages, c.n_slots, n_seqs), Requests{slots, nullptr, add, n_seqs}, static_cast<hipStream_t>(stream));
     return launched();
 }
 
@@ -724,16 +890,10 @@ extern "C" lq_status lora_cache_fork(const lq_cache* host_cache, const int32_t* 
     const lq_status st = page_call(host_cache, n_seqs, workspace, workspace_bytes, &c);
     if (st != LQ_OK || n_seqs == 0) return st;
     const PagePlan p = plan_of(workspace, c.n_pages, c.n_slots, n_seqs);
-    const int n_seg = segments_of(c.n_pages);
-    const int waves = kPlanThreads / kWave;
     const hipStream_t hs = static_cast<hipStream_t>(stream);
-    hipLaunchKernelGGL(plan_kernel<true>, dim3(1 + n_seg), dim3(kPlanThreads), 0, hs, c, p, Requests{src_slots, dst_slots, keep, n_seqs});
-    hipLaunchKernelGGL(assign_kernel<true>, dim3(n_seg + (n_seqs + waves - 1) / waves), dim3(kPlanThreads), 0, hs, c, p, n_seqs, n_seg);
-    if (n_pools > 0) {
-        const long long most = (long long)n_seqs * n_pools * ((c.page_bytes + kCopyBytes - 1) / kCopyBytes);
-        hipLaunchKernelGGL(copy_pages_kernel, dim3(copy_grid(most)), dim3(kCopyThreads), 0, hs, c, p.from, p.page, nullptr, n_seqs, pools,
-                           n_pools);
-    }
+    plan_and_assign<true>(c, p, Requests{src_slots, dst_slots, keep, n_seqs}, hs);
+    const int waves = kCopyThreads / kWave, n_state = (n_seqs + waves - 1) / waves;
+    hipLaunchKernelGGL(fork_kernel, dim3(n_state + copy_groups(c, n_seqs, n_pools)), dim3(kCopyThreads), 0, hs, c, p, n_seqs, n_state, pools, n_pools);
     return launched();
 }
 
@@ -745,7 +905,7 @@ extern "C" lq_status lora_cache_free(const lq_cache* host_cache, const int32_t* 
     if (n_seqs > 0 && !slots) return LQ_ERR_INVALID_ARG;
     const lq_status st = page_call(host_cache, n_seqs, workspace, workspace_bytes, &c);
     if (st != LQ_OK || n_seqs == 0) return st;
-    hipLaunchKernelGGL(free_kernel, dim3(n_seqs), dim3(kPlanThreads), 0, static_cast<hipStream_t>(stream), c, slots);
+    hipLaunchKernelGGL(free_kernel, dim3(n_seqs), dim3(kSegThreads), 0, static_cast<hipStream_t>(stream), c, slots);
     return launched();
 }
 
@@ -758,17 +918,15 @@ extern "C" lq_status lora_cache_compact(const lq_cache* host_cache, void* const*
     const lq_status st = page_call(host_cache, 0, workspace, workspace_bytes, &c);
     if (st != LQ_OK) return st;
     const PagePlan p = plan_of(workspace, c.n_pages, c.n_slots, 0);
-    const int n_seg = segments_of(c.n_pages);
     const hipStream_t hs = static_cast<hipStream_t>(stream);
-    hipLaunchKernelGGL(count_live_kernel, dim3(n_seg), dim3(kPlanThreads), 0, hs, c, p);
-    hipLaunchKernelGGL(list_moves_kernel, dim3(n_seg), dim3(kPlanThreads), 0, hs, c, p, n_seg);
-    const int ref_groups = n_seg < 64 ? n_seg : 64;
-    hipLaunchKernelGGL(follow_moves_kernel, dim3(ref_groups + c.n_slots), dim3(kPlanThreads), 0, hs, c, p, ref_groups, n_live);
-    if (n_pools > 0) {
-        const long long most = ((long long)c.n_pages / 2 + 1) * n_pools * ((c.page_bytes + kCopyBytes - 1) / kCopyBytes);
-        hipLaunchKernelGGL(copy_pages_kernel, dim3(copy_grid(most)), dim3(kCopyThreads), 0, hs, c, p.list_src, p.list_dst, p.totals, 0, pools,
-                           n_pools);
+    if (c.n_pages <= kSmallPages) hipLaunchKernelGGL(list_small_kernel, dim3(1), dim3(kPlanThreads), 0, hs, c, p);
+    else {
+        const int n_seg = segments_of(c.n_pages);
+        hipLaunchKernelGGL(count_live_kernel, dim3(n_seg), dim3(kSegThreads), 0, hs, c, p);
+        hipLaunchKernelGGL(list_moves_kernel, dim3(n_seg), dim3(kSegThreads), 0, hs, c, p, n_seg);
     }
+    hipLaunchKernelGGL(compact_kernel, dim3(kRefGroups + c.n_slots + copy_groups(c, c.n_pages / 2 + 1, n_pools)), dim3(kCopyThreads), 0, hs, c, p, n_live, pools,
+                       n_pools);
     return launched();
 }
 

@@ -356,7 +356,8 @@ def assert_pages(cache, model, marks=True):
             assert (got[torch.from_numpy(live).cuda()] == want[:, None]).all()
 
 
-@pytest.mark.parametrize("seed,n_pages,n_slots,max_pages,T", [(0, 40, 12, 8, 16), (1, 300, 40, 20, 32), (2, 9000, 300, 64, 16)])
+@pytest.mark.parametrize("seed,n_pages,n_slots,max_pages,T", [(0, 40, 12, 8, 16), (1, 300, 40, 20, 32), (2, 9000, 300, 64, 16),
+                                                                  (3, 8000, 9000, 12, 16), (4, 20000, 9000, 16, 16)])
 def test_page_calls_against_the_model(seed, n_pages, n_slots, max_pages, T):
     """A random program of reserve, fork, free and compact, with requests that cannot be served among them."""
     rng = np.random.default_rng(seed)
