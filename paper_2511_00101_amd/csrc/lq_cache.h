@@ -50,25 +50,18 @@ __device__ __forceinline__ Span load_span(const CacheView& c, const Spans& p, in
     return u;
 }
 
-// The largest s with key(s) <= i, or -1; key does not decrease over 0 .. n - 1.  Every lane of the wave gets it.  Up to 512 keys are all
+// The largest s with key(s) <= i, or -1; key does not decrease over 0 .. n - 1.  Every lane of the wave gets it.  Up to 256 keys are all
 // looked at, in one round trip; of more, 64 a round.
 template <class Key>
 __device__ __forceinline__ int last_not_above(int n, int i, Key&& key)
 {
-    constexpr int AT_ONCE = 8;
+    constexpr int AT_ONCE = 4;
     if (n <= AT_ONCE * kWave) {
-        bool below[AT_ONCE];
-        int found = 0;
+        int k[AT_ONCE], found = 0;
 #pragma unroll
-        for (int k = 0; k < AT_ONCE; ++k) {
-            below[k] = false;
-            if (k * kWave < n) {
-                const int s = k * kWave + lane_id();
-                below[k] = key(min(s, n - 1)) <= i && s < n;
-            }
-        }
+        for (int r = 0; r < AT_ONCE; ++r) k[r] = key(min(r * kWave + lane_id(), n - 1));      // (no branch: the loads go out together)
 #pragma unroll
-        for (int k = 0; k < AT_ONCE; ++k) found += __popcll(__ballot(below[k]));
+        for (int r = 0; r < AT_ONCE; ++r) found += __popcll(__ballot(bool(r * kWave + lane_id() < n) & bool(k[r] <= i)));
         return found - 1;
     }
     int at = 0, width = n;      // the answer lies in [at - 1, at + width)

@@ -56,27 +56,35 @@ __device__ __forceinline__ bool find_block(const CacheView& c, const Spans& sp, 
     if (s < 0) return false;
     j.slot = sp.slots ? sp.slots[s] : s;
     j.row0 = sp.row_starts[s];
-    const int end = sp.row_starts[s + 1];
+    int end = sp.row_starts[s + 1];
     j.first = sp.first[s];
-    j.rows_ok = j.row0 >= 0 && end >= j.row0 && end <= sp.n_rows;
+    // (lane 0's values, read here: the loads are one round trip, none of them moved behind a branch)
+    j.slot = uniform(j.slot);
+    j.row0 = uniform(j.row0);
+    end = uniform(end);
+    j.first = uniform(j.first);
+    j.rows_ok = bool(j.row0 >= 0) & bool(end >= j.row0) & bool(end <= sp.n_rows);
     j.n = j.rows_ok ? end - j.row0 : 0;
     const int local = item - ((j.row0 >> 4) + 2 * s);
-    const bool reach = j.first >= 0 && j.n <= c.max_len - j.first;
-    // (a span that cannot be used is reported by the wave of its first item)
+    const bool reach = bool(j.first >= 0) & bool(j.n <= c.max_len - j.first);
     if (local < 0) return false;                       // (row_starts that decrease)
+    // (a span that cannot be used is reported by the wave of its first item)
     if (local > 0 && (!j.rows_ok || !reach || local > ((j.first + j.n - 1) >> 4) - (j.first >> 4))) return false;
     if (j.rows_ok && j.n == 0) return false;
-    if (!reach) j.rows_ok = false;
+    j.rows_ok = j.rows_ok & reach;
     j.pos0 = j.rows_ok ? ((j.first >> 4) + local) * kBlock : 0;
     const int slot = min(max(j.slot, 0), c.n_slots - 1);
     j.len = c.lens[slot];
     j.page = c.table[(long long)slot * c.max_pages + (j.pos0 >> c.t_log2)];
-    if (j.slot != slot) j.rows_ok = false;
+    j.rows_ok = j.rows_ok & bool(j.slot == slot);
     return true;
 }
-__device__ __forceinline__ bool usable(const CacheView& c, const BlockJob& j)
+__device__ __forceinline__ bool usable(const CacheView& c, BlockJob& j)
 {
-    return j.rows_ok && j.len >= 0 && j.len <= c.max_len && j.first <= j.len && j.n <= j.len - j.first && j.page >= 0 && j.page < c.n_pages;
+    j.len = uniform(j.len);
+    j.page = uniform(j.page);
+    return j.rows_ok & bool(j.len >= 0) & bool(j.len <= c.max_len) & bool(j.first <= j.len) & bool(j.n <= j.len - j.first) & bool(j.page >= 0) &
+           bool(j.page < c.n_pages);
 }
 
 template <int N>
@@ -92,16 +100,58 @@ struct Packed {                                  // N = 4 or 8 consecutive bf16 
             w[0] = v.x; w[1] = v.y;
         }
     }
+    // here the loads are waited for (and not behind a branch that they were moved across)
+    __device__ __forceinline__ void arrive()
+    {
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) asm volatile("" : "+v"(w[i]));
+    }
     __device__ __forceinline__ float at(int i) const { return i % 2 ? bf16_hi(w[i / 2]) : bf16_lo(w[i / 2]); }
 };
 
+// N words at a time: 1, 2, 4 or 8
+template <int N>
+__device__ __forceinline__ void load_words(const uint8_t* p, unsigned int (&w)[N])
+{
+    if constexpr (N == 1) w[0] = *reinterpret_cast<const unsigned int*>(p);
+    else if constexpr (N == 2) {
+        const u32x2 v = *reinterpret_cast<const u32x2*>(p);
+        w[0] = v.x; w[1] = v.y;
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            const u32x4 v = *reinterpret_cast<const u32x4*>(p + 4 * i);
+            w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
+        }
+    }
+}
+template <int N>
+__device__ __forceinline__ void store_words(uint8_t* p, const unsigned int (&w)[N])
+{
+    if constexpr (N == 1) *reinterpret_cast<unsigned int*>(p) = w[0];
+    else if constexpr (N == 2) *reinterpret_cast<u32x2*>(p) = u32x2{w[0], w[1]};
+    else {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) *reinterpret_cast<u32x4*>(p + 4 * i) = u32x4{w[i], w[i + 1], w[i + 2], w[i + 3]};
+    }
+}
+
 __device__ __forceinline__ bool finite(float v) { return fabsf(v) < __builtin_inff(); }
 
+// largest of the wave's values, in every lane: rotations within rows of 16 lanes, then rows and halves swapped
 __device__ __forceinline__ float wave_max(float v)
 {
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) v = fmaxf(v, __shfl_xor(v, d, kWave));
-    return v;
+    typedef __attribute__((ext_vector_type(2))) unsigned int pair;
+#define LQ_ROTATED(n) __uint_as_float((unsigned int)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x120 + (n), 0xf, 0xf, false))
+    v = fmaxf(v, LQ_ROTATED(1));
+    v = fmaxf(v, LQ_ROTATED(2));
+    v = fmaxf(v, LQ_ROTATED(4));
+    v = fmaxf(v, LQ_ROTATED(8));
+#undef LQ_ROTATED
+    const pair a = __builtin_bit_cast(pair, __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false));
+    v = fmaxf(__uint_as_float(a.x), __uint_as_float(a.y));
+    const pair b = __builtin_bit_cast(pair, __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false));
+    return fmaxf(__uint_as_float(b.x), __uint_as_float(b.y));
 }
 
 // least e with amax <= 448 * 2^e (448 = 1.75 * 2^8), within [-100, 119]
@@ -157,6 +207,11 @@ __global__ __launch_bounds__(256) void store_rows_kernel(CacheView c, Spans sp, 
         kv[0][t].load(k + row * ldk + head * HD + m * D);
         kv[1][t].load(v + row * ldv + head * HD + m * D);
     }
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        kv[0][t].arrive();
+        kv[1][t].arrive();
+    }
     if (!usable(c, j)) {
         if (lane == 0) atomicOr(c.err, kErrBadSegment);
         return;
@@ -173,11 +228,8 @@ __global__ __launch_bounds__(256) void store_rows_kernel(CacheView c, Spans sp, 
     if (has_old) {
         old_e = *reinterpret_cast<const u16*>(se);
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int i = 0; i < W; ++i) old_k[t][i] = reinterpret_cast<const unsigned int*>(kc + t * HD)[i];
-#pragma unroll
-        for (int d = 0; d < D; ++d) old_v[d] = reinterpret_cast<const unsigned int*>(vc)[d];
+        for (int t = 0; t < 4; ++t) load_words(kc + t * HD, old_k[t]);
+        load_words(vc, old_v);
     }
     float amax[2] = {0.f, 0.f};
 #pragma unroll
@@ -187,12 +239,9 @@ __global__ __launch_bounds__(256) void store_rows_kernel(CacheView c, Spans sp, 
 #pragma unroll
             for (int d = 0; d < D; ++d) {
                 const float f = kv[x][t].at(d);
-                amax[x] = fmaxf(amax[x], (is_new >> t & 1u) && finite(f) ? fabsf(f) : 0.f);
+                const bool counts = bool(is_new >> t & 1u) & finite(f);
+                amax[x] = fmaxf(amax[x], counts ? fabsf(f) : 0.f);
             }
-    if (refs != 1) {
-        if (lane == 0) atomicOr(c.err, kErrBadSegment);
-        return;
-    }
     int e[2], e_old[2];
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
@@ -204,43 +253,53 @@ __global__ __launch_bounds__(256) void store_rows_kernel(CacheView c, Spans sp, 
 #pragma unroll
     for (int t = 0; t < 4; ++t) is_old |= pos + t < j.first ? 1u << t : 0u;
 
+    const float r[2] = {block_scale((unsigned)(127 - e[0])), block_scale((unsigned)(127 - e[1]))};
+    // the kept codes at the new exponents (positions behind the last row, which share a word of V with others, are nobody's)
+    const bool again[2] = {has_old && e[0] != e_old[0], has_old && e[1] != e_old[1]};      // wave uniform
+    if (again[0]) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                float f[4];
+                decode4(old_k[t][i], block_scale((unsigned)(127 + e_old[0])), f);
+                old_k[t][i] = encode4(f, r[0]);
+            }
+    }
+    if (again[1]) {
+#pragma unroll
+        for (int d = 0; d < D; ++d) {
+            float f[4];
+            decode4(old_v[d], block_scale((unsigned)(127 + e_old[1])), f);
+            old_v[d] = encode4(f, r[1]);
+        }
+    }
+    if (refs != 1) {                            // a shared page
+        if (lane == 0) atomicOr(c.err, kErrBadSegment);
+        return;
+    }
     // K: a position's codes are contiguous
-    const float rk = block_scale((unsigned)(127 - e[0])), rv = block_scale((unsigned)(127 - e[1]));
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-        const bool again = (is_old >> t & 1u) && e[0] != e_old[0];
-        if (!(is_new >> t & 1u) && !again) continue;
+        const bool fresh = is_new >> t & 1u;
         unsigned int w[W];
 #pragma unroll
         for (int i = 0; i < W; ++i) {
-            float f[4];
-            if (again) {
-                decode4(old_k[t][i], block_scale((unsigned)(127 + e_old[0])), f);
-                w[i] = encode4(f, rk);
-            } else {
-                const float f4[4] = {kv[0][t].at(4 * i), kv[0][t].at(4 * i + 1), kv[0][t].at(4 * i + 2), kv[0][t].at(4 * i + 3)};
-                w[i] = encode4(f4, rk);
-            }
+            const float f[4] = {kv[0][t].at(4 * i), kv[0][t].at(4 * i + 1), kv[0][t].at(4 * i + 2), kv[0][t].at(4 * i + 3)};
+            const unsigned int code = encode4(f, r[0]);
+            w[i] = fresh ? code : old_k[t][i];
         }
-#pragma unroll
-        for (int i = 0; i < W; ++i) reinterpret_cast<unsigned int*>(kc + t * HD)[i] = w[i];
+        if (fresh || (again[0] && (is_old >> t & 1u))) store_words(kc + t * HD, w);
     }
     // V: a word holds four positions of a column
     const unsigned int sel = (is_new & 1u ? 0xffu : 0u) | (is_new & 2u ? 0xff00u : 0u) | (is_new & 4u ? 0xff0000u : 0u) | (is_new & 8u ? 0xff000000u : 0u);
-    const bool again = is_old && e[1] != e_old[1];
-    if (is_new || again) {
+    unsigned int w[D];
 #pragma unroll
-        for (int d = 0; d < D; ++d) {
-            unsigned int old = old_v[d];        // (positions behind the last row: nobody's)
-            if (again) {
-                float f[4];
-                decode4(old, block_scale((unsigned)(127 + e_old[1])), f);
-                old = encode4(f, rv);
-            }
-            const float f[4] = {kv[1][0].at(d), kv[1][1].at(d), kv[1][2].at(d), kv[1][3].at(d)};
-            reinterpret_cast<unsigned int*>(vc)[d] = (encode4(f, rv) & sel) | (old & ~sel);
-        }
+    for (int d = 0; d < D; ++d) {
+        const float f[4] = {kv[1][0].at(d), kv[1][1].at(d), kv[1][2].at(d), kv[1][3].at(d)};
+        w[d] = (encode4(f, r[1]) & sel) | (old_v[d] & ~sel);
     }
+    if (is_new || (is_old && again[1])) store_words(vc, w);
     if (lane < 2) se[lane] = (uint8_t)((lane == 0 ? e[0] : e[1]) + 127);
 }
 
@@ -267,13 +326,10 @@ __global__ __launch_bounds__(256) void load_rows_kernel(CacheView c, Spans sp, c
     const uint8_t* se = page + c.scale_off + (head * (T / kBlock) + in_page / kBlock) * 2;
     unsigned int kw[4][W];
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int w = 0; w < W; ++w) kw[t][w] = reinterpret_cast<const unsigned int*>(kc + t * HD)[w];
+    for (int t = 0; t < 4; ++t) load_words(kc + t * HD, kw[t]);
     const float sk = block_scale(se[0]), sv = block_scale(se[1]);
     unsigned int vw[D];
-#pragma unroll
-    for (int d = 0; d < D; ++d) vw[d] = reinterpret_cast<const unsigned int*>(vc)[d];
+    load_words(vc, vw);
     float vf[D][4];
 #pragma unroll
     for (int d = 0; d < D; ++d) decode4(vw[d], sv, vf[d]);
@@ -284,13 +340,18 @@ __global__ __launch_bounds__(256) void load_rows_kernel(CacheView c, Spans sp, c
         const long long row = j.row0 + i;
         u16* ko = k + row * ldk + head * HD + m * D;
         u16* vo = v + row * ldv + head * HD + m * D;
+        unsigned int wk[D / 2], wv[D / 2];
 #pragma unroll
         for (int w = 0; w < W; ++w) {
             float f[4];
             decode4(kw[t][w], sk, f);
-            reinterpret_cast<u32x2*>(ko)[w] = u32x2{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3])};
-            reinterpret_cast<u32x2*>(vo)[w] = u32x2{pack_bf16x2(vf[4 * w][t], vf[4 * w + 1][t]), pack_bf16x2(vf[4 * w + 2][t], vf[4 * w + 3][t])};
+            wk[2 * w] = pack_bf16x2(f[0], f[1]);
+            wk[2 * w + 1] = pack_bf16x2(f[2], f[3]);
+            wv[2 * w] = pack_bf16x2(vf[4 * w][t], vf[4 * w + 1][t]);
+            wv[2 * w + 1] = pack_bf16x2(vf[4 * w + 2][t], vf[4 * w + 3][t]);
         }
+        store_words(reinterpret_cast<uint8_t*>(ko), wk);
+        store_words(reinterpret_cast<uint8_t*>(vo), wv);
     }
 }
 
