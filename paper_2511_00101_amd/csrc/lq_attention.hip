@@ -31,7 +31,8 @@ constexpr int kArrivalBytes = kWsHeaderBytes - 4 * kArrivals;
 template <int NT> constexpr int kSlots = NT <= 2 ? 4 * kArrivalBytes : 2 * kArrivalBytes;
 constexpr int kManyChunksSlots = 2 * kArrivalBytes;    // with counters of eight bits
 template <int HD, int NT> constexpr int kResident = HD == 64 ? (NT == 1 ? 4 : NT == 2 ? 3 : 2) : NT == 1 ? 3 : 2;   // workgroups of a CU
-constexpr int kLeastChunk = 2 * kRound;
+constexpr int kLeastChunk = 4 * kRound;
+constexpr int kAloneLongest = kLeastChunk;      // (not split, then)
 constexpr int kClasses = 5;
 constexpr int kKeptSpans = 1024;                // spans that a workgroup keeps in LDS (16 KB); of more, a unit's is read again
 __host__ __device__ constexpr int span_at(int n) { return (3 * n + 1 + 3) / 4 * 4; }
@@ -217,6 +218,7 @@ struct Attention {
     struct State { f32x4 o[NT][D]; float m[NT], l[NT]; };
 
     struct Scores { f32x4 s[2][NT]; };
+    static constexpr bool kAlone = NT == 1;     // a unit per wave is offered
     static constexpr bool kSharedQ = NT >= 4;   // Q's fragments in LDS (the waves have the same rows): 64 registers less
     // Prompts with head_dim 128: K's codes are the operand themselves, with their block's exponent as the matrix instruction's scale, and a row of Q
     // is two rows of codes under one exponent e: q = 2^e (high + low / 16).  A bf16 value's eight bits are a four-bit high part and a four-bit
@@ -366,11 +368,12 @@ struct Attention {
     };
 
     // probabilities of a step, and its share of O^T
-    // request() is called halfway, when half of the scores' registers are free
+    // request() is called halfway, when half of the scores' registers are free; with one row tile at once
     template <class Request>
     static __device__ __forceinline__ void accumulate(Request&& request, const u32x4 (&v)[2][LD], bool ok0, bool ok1, Scores& scores, const unsigned int (&e)[2],
                                                       const Rows& rows, int key0, int last_key, bool masked, float c_log2, State& st)
     {
+        if (NT == 1) request();
         const bool ok[2] = {ok0, ok1};
         const int kg = lane_id() >> 4;
         f32x4 (&sc)[2][NT] = scores.s;
@@ -501,10 +504,12 @@ struct Attention {
                 add(n + 1, 7);
                 pack(n + 1, 6);
             }
-            if (n == NT / 2 - 1) request();
+            if (NT > 1 && n == NT / 2 - 1) request();
         }
     }
 
+    // ALONE: the wave has the unit to itself (no other wave of the workgroup may be waited for)
+    template <bool ALONE>
     static __device__ __forceinline__ void run_unit(const AttnParams& p, const Unit& u, int chunk_len, Shared& sh)
     {
         const CacheView& c = p.c;
@@ -566,7 +571,8 @@ struct Attention {
         if (kSharedQ) __syncthreads();
         const int q_exp = kCodesQ ? *reinterpret_cast<const int*>(sh.q_exp[col]) : 0;
 
-        int key = begin + wave * kStep;
+        constexpr int stride = ALONE ? kStep : kRound;
+        int key = begin + (ALONE ? 0 : wave * kStep);
         if (key < end) {
             PageIds ids;
             ids.start(c.table + (long long)u.slot * c.max_pages, (last_key >> c.t_log2) + 1, key >> c.t_log2);
@@ -579,42 +585,44 @@ struct Attention {
             load_k(w, s);
             load_v(p, w, s);
             const auto is_masked = [&](const Step<HD>& t) { return key + kStep - 1 > first_pos || !t.ok[0] || !t.ok[1]; };
-            if constexpr (NT >= 4) {
-                // K is free for the next step's codes once the scores are there, V at the step's end (behind the last step the
-                // same codes are requested again: no branch)
-                for (; key < end; key += kRound) {
-                    const int next = key + kRound < end ? key + kRound : key;
-                    const bool masked = is_masked(s), ok0 = s.ok[0], ok1 = s.ok[1];
-                    const unsigned int e[2] = {(unsigned)uniform((int)s.e[0]), (unsigned)uniform((int)s.e[1])};
-                    w = find_step(hd, ids, next, last_key, bad);
-                    Scores sc;
-                    __builtin_amdgcn_s_setprio(1);      // (the other wave of the SIMD has exponentials to do)
-                    scores(s, q, q_exp, sh, sc);
-                    __builtin_amdgcn_s_setprio(0);
-                    accumulate([&] { load_k(w, s); }, s.v, ok0, ok1, sc, e, tr, key, last_key, masked, p.c_log2, st);
-                    load_v(p, w, s);
-                }
-            } else {
-                // memory bound: all of the next step's codes are requested a step ahead
-                while (true) {
-                    const int next = key + kRound;
-                    Step<HD> ahead = s;
-                    if (next < end) {
-                        w = find_step(hd, ids, next, last_key, bad);
-                        load_k(w, ahead);
-                        load_v(p, w, ahead);
-                    }
-                    Scores sc;
-                    scores(s, q, q_exp, sh, sc);
-                    accumulate([] {}, s.v, s.ok[0], s.ok[1], sc, s.e, tr, key, last_key, is_masked(s), p.c_log2, st);
-                    if (next >= end) break;
-                    key = next;
-                    s = ahead;
-                }
+            // K's registers are free for the next step's codes once the scores are there, V's at the step's end.  A second set of registers,
+            // requested a whole step ahead, was slower: what it spilled cost more (decode of 256 requests 145 us against 138).  Behind
+            // the last step long row tiles request the same codes again, which spares their loop the branches.
+            for (; key < end; key += stride) {
+                const int next = key + stride;
+                const bool more = NT >= 4 || next < end;
+                const bool masked = is_masked(s), ok0 = s.ok[0], ok1 = s.ok[1];
+                const unsigned int e[2] = {(unsigned)uniform((int)s.e[0]), (unsigned)uniform((int)s.e[1])};
+                if (more) w = find_step(hd, ids, next < end ? next : key, last_key, bad);
+                Scores sc;
+                __builtin_amdgcn_s_setprio(1);      // (the other waves of the SIMD have exponentials to do)
+                scores(s, q, q_exp, sh, sc);
+                __builtin_amdgcn_s_setprio(0);
+                accumulate([&] { if (more) load_k(w, s); }, s.v, ok0, ok1, sc, e, tr, key, last_key, masked, p.c_log2, st);
+                if (more) load_v(p, w, s);
             }
             if (bad && lane == 0) atomicOr(c.err, kErrBadSegment);
         }
         if (kSharedQ) __syncthreads();          // acc takes q's place
+
+        if constexpr (ALONE) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const int x = 16 * n + col;
+                const float l = column_sum(st.l[n]), inv = l == 0.f ? 0.f : 1.f / l;
+                if (x >= tr.left) continue;
+                int token, h;
+                row_of(x, token, h);
+                u16* dst = p.out + (long long)(u.row0 + token) * p.ldo + h * HD + 16 * kg;
+#pragma unroll
+                for (int i = 0; i < D; i += 4)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        *reinterpret_cast<u32x2*>(dst + 16 * i + 4 * r) = u32x2{pack_bf16x2(st.o[n][i][r] * inv, st.o[n][i + 1][r] * inv),
+                                                                                pack_bf16x2(st.o[n][i + 2][r] * inv, st.o[n][i + 3][r] * inv)};
+            }
+            return;
+        }
 
         // the waves' maxima and sums
 #pragma unroll
@@ -873,7 +881,13 @@ __global__ __launch_bounds__(kAttnThreads, (kResident<HD, NT>)) void attention_k
     if (threadIdx.x == 0) units[n] = unit_base;
     __syncthreads();
 
-    for_each_unit(p.tickets, uniform(unit_base) * heads, sh.slot, [&](int id, int) {
+    // Many short sequences: a unit per wave.  (A unit's instructions outside its steps, some 1000 a wave, are then spent by one wave and not
+    // by four, and nothing is exchanged.)
+    const int n_units = uniform(unit_base) * heads;
+    const bool alone = A::kAlone && uniform(longest) <= kAloneLongest && n_units > (int)gridDim.x;
+    for_each_unit(p.tickets, alone ? (n_units + kAttnWaves - 1) / kAttnWaves : n_units, sh.slot, [&](int group, int) {
+        const int id = alone ? group * kAttnWaves + uniform((int)threadIdx.x / kWave) : group;
+        if (id >= n_units) return;
         Unit u;
         const int v = id / heads;
         u.head = id - v * heads;
@@ -891,7 +905,13 @@ __global__ __launch_bounds__(kAttnThreads, (kResident<HD, NT>)) void attention_k
         u.chunk = local - back * u.chunks;
         u.tile = tiles_of(Span{u.slot, u.row0, u.n, u.first}) - 1 - back;      // the tiles with the most positions first
         u.slot0 = ((uniform(slots[at]) + back * u.chunks) * heads + u.head * u.chunks);
-        A::run_unit(p, u, chunk_len, sh);
+        if constexpr (A::kAlone) {
+            if (alone) {
+                A::template run_unit<true>(p, u, chunk_len, sh);
+                return;
+            }
+        }
+        A::template run_unit<false>(p, u, chunk_len, sh);
     });
 }
 
