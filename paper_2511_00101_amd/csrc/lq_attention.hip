@@ -235,9 +235,9 @@ struct Attention {
         for (int i = 0; i < 4; ++i) unpack8(w[i], x + 8 * i);
 #pragma unroll
         for (int i = 0; i < 32; ++i) amax = fmaxf(amax, fabsf(x[i]));
-        amax = column_max(amax);                                       // (an infinity is 448 and more: its code is made NaN below)
-        const unsigned int u = __float_as_uint(fminf(amax, 3e38f));
-        const int e = min(max((int)(u >> 23) - 127 - ((u & 0x7fffffu) <= 0x600000u ? 8 : 7), -100), 119);   // least with amax <= 448 * 2^e
+        amax = column_max(amax);
+        const unsigned int u = __float_as_uint(fminf(amax, 3.4e38f));
+        const int e = max((int)(u >> 23) - 127 - ((u & 0x7fffffu) <= 0x600000u ? 8 : 7), -118);   // least with amax <= 448 * 2^e
         const float r = __uint_as_float((unsigned)(127 - e) << 23);
         exponent = (unsigned)(e + 127);                                // E8M0, of the high parts; the low parts' is 4 less
 #pragma unroll
@@ -246,11 +246,9 @@ struct Attention {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 float a[2], rest[2];
+                // (an infinity becomes NaN with the conversion, as its row's scores would)
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const float v = x[4 * i + 2 * h + k];
-                    a[k] = fabsf(v) < __builtin_inff() ? fminf(fmaxf(v * r, -448.f), 448.f) : __builtin_nanf("");
-                }
+                for (int k = 0; k < 2; ++k) a[k] = x[4 * i + 2 * h + k] * r;
                 const unsigned int code = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(a[0], a[1], 0, false) & 0xffffu;
                 const f32x2 back = __builtin_amdgcn_cvt_pk_f32_fp8((int)code, false);
 #pragma unroll
@@ -823,7 +821,7 @@ __global__ __launch_bounds__(kAttnThreads, (kResident<HD, NT>)) void attention_k
     const auto length = [&](int n_slots, int most) { return max((work + n_slots / 2 - 1) / (n_slots / 2), (long long)((longest + most - 1) / most)); };
     const long long few = length(kSlots<NT>, 15), many = length(kManyChunksSlots, 255);
     const int bits = uniform(few <= many ? 4 : 8);
-    const long long round = work * 2 / (int)gridDim.x + 1;            // half a unit per workgroup
+    const long long round = work * (NT >= 4 ? 3 : 2) / (int)gridDim.x + 1;   // a third, half a unit per workgroup
     const long long len = max(max(min(few, many), round), (long long)kLeastChunk);
     const int chunk_len = uniform((int)min((len + kRound - 1) / kRound * kRound, 1ll << 30));
 
