@@ -935,11 +935,15 @@ hipError_t launch_attention(AttnParams p, int max_units, void* workspace, hipStr
     return hipGetLastError();
 }
 
-// row tiles of 16: a group of query heads of one token, a draft, or a prompt
-int row_tiles(int group, int max_rows)
+// Row tiles of 16 of a unit: a group of query heads of one token, a draft, or a prompt.  Four tiles widen every code for 64 rows and
+// cost 5 us to set up and to join; up to 128 rows in all, units of two tiles are faster while they fill the chip's compute units no more
+// than three times (us, two tiles against four: 20 spans of 16 rows of 4 heads 9 against 12; one of 31 x 3 rows behind 18444 positions 29 against 44;
+// but 60 spans of 14 x 3 rows for 16 key heads, 1920 units, 33 against 25).
+int row_tiles(int group, int max_rows, int n_seqs, int kv_heads)
 {
     const long long rows = (long long)group * max_rows;
-    return rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    if (rows <= 16) return 1;
+    return rows <= 32 || (rows <= 128 && (rows + 31) / 32 * n_seqs * kv_heads <= 768) ? 2 : 4;
 }
 
 }  // namespace
@@ -949,8 +953,10 @@ extern "C" size_t lora_cache_attention_workspace_bytes(const lq_cache* host_cach
 {
     using namespace lq;
     if (!host_cache || host_cache->n_kv_heads <= 0 || n_heads <= 0 || n_heads % host_cache->n_kv_heads || max_rows <= 0) return 0;
-    const int nt = row_tiles(n_heads / host_cache->n_kv_heads, max_rows);
-    const size_t slots = nt <= 2 ? kSlots<2> : kSlots<4>;
+    // (two row tiles and four need the same)
+    static_assert(kSlots<2> * 2 == kSlots<4> * 4, "one size for both");
+    const int nt = row_tiles(n_heads / host_cache->n_kv_heads, max_rows, 1, 1);
+    const size_t slots = nt == 1 ? kSlots<1> : nt == 2 ? kSlots<2> : kSlots<4>;
     return kWsHeaderBytes + slots * 16 * nt * ((size_t)host_cache->head_dim + 2) * 4;
 }
 
@@ -986,7 +992,7 @@ extern "C" lq_status lora_cache_attention(const void* q, int64_t ldq, void* out,
     p.c_log2 = __builtin_fmaxf(__builtin_fabsf(scale) * 1.44269504f, 1e-30f);
     p.group_magic = (unsigned)(((1 << 20) + p.group - 1) / p.group);
     p.q_sign = scale < 0.f ? 0x80008000u : 0u;
-    const int nt = row_tiles(p.group, max_rows);
+    const int nt = row_tiles(p.group, max_rows, n_seqs, kv);
     // no more workgroups than there can be units
     const int64_t tiles = (int64_t)n_rows * p.group / (16 * nt) + n_seqs;
     const int64_t chunks = (p.c.max_len + kLeastChunk - 1) / kLeastChunk;

@@ -210,6 +210,16 @@ ATTENTION = [
     (2, 1, 128, 16, [(9, 1)] * 70, 4),                           # more spans than a wave has lanes
     (1, 1, 64, 16, [(20000, 1)], 1),                             # a long axis and nothing else to spread
     (5, 5, 128, 64, [(6000, 2), (3, 2)], 2),
+    (8, 4, 64, 16, [(i % 37, 1) for i in range(300)], 1),        # more units than workgroups: a unit per wave; more spans than threads
+    (4, 2, 128, 16, [(i * 7 % 90, 1) for i in range(450)], 1),
+    (2, 1, 64, 16, [(i % 5, 1) for i in range(1100)], 1),        # more spans than are kept
+    (4, 2, 128, 16, [(5000, 3), (2500, 1), (1, 2)], 3),          # pages beyond a wave's first 64, chunks in byte counters
+    (8, 2, 128, 64, [(3000, 1), (3100, 1)] + [(900, 1)] * 10, 1),   # chunks in four-bit counters
+    (6, 1, 128, 32, [(4000, 5), (10, 5)], 5),                    # a draft split
+    (4, 1, 64, 16, [(2600, 40), (0, 40)], 40),                   # a prompt split
+    (8, 1, 128, 128, [(1500, 20), (2047, 1)], 20),
+    (16, 1, 128, 16, [(700, 8)], 8),                             # 128 rows: four units of two tiles
+    (12, 4, 64, 32, [(3, 14), (60, 13)] * 36, 14),               # few rows, many units: four tiles
 ]
 
 
