@@ -80,6 +80,13 @@ __device__ __forceinline__ bf16x8 eight_bf16(unsigned int a, float sa, unsigned 
 }
 __device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
+// Two bf16 values with an infinity made NaN: its row's scores may all be minus infinity, which a sum of exponentials does not tell from
+// a row that sees nothing.
+__device__ __forceinline__ unsigned int no_infinities(unsigned int w)
+{
+    return w | (((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u) >> 9;
+}
+
 // all ones where a row that sees positions up to `limit` does not see `key` (in integers: comparisons would hold a mask
 // register pair per element)
 __device__ __forceinline__ unsigned int hidden(int limit, int key, bool ok) { return (unsigned int)(((ok ? limit : -1) - key) >> 31); }
@@ -246,7 +253,6 @@ struct Attention {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 float a[2], rest[2];
-                // (an infinity becomes NaN with the conversion, as its row's scores would)
 #pragma unroll
                 for (int k = 0; k < 2; ++k) a[k] = x[4 * i + 2 * h + k] * r;
                 const unsigned int code = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(a[0], a[1], 0, false) & 0xffffu;
@@ -546,7 +552,8 @@ struct Attention {
             for (int j = 0; j < HD / 32; ++j) {
                 w[j] = u32x4{0, 0, 0, 0};
                 if (r < rows) w[j] = *reinterpret_cast<const u32x4*>(src + (j / 2) * 64 + (j % 2) * 8);
-                w[j].x ^= p.q_sign; w[j].y ^= p.q_sign; w[j].z ^= p.q_sign; w[j].w ^= p.q_sign;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[j][i] = no_infinities(w[j][i] ^ p.q_sign);
             }
             if constexpr (kCodesQ) {
                 u32x4 high[2], low[2];

@@ -97,7 +97,8 @@ def test_row_calls_refuse_before_launching(lq):
     for bad in (dict(q=None), dict(out=None), dict(out=ONE), dict(ldq=248), dict(ldo=128), dict(heads=3), dict(heads=0), dict(max_rows=0),
                 dict(scale=float("nan")), dict(scale=float("inf")), dict(pages=None), dict(n_rows=-1)):
         assert attend(**bad) == lq.LQ_ERR_INVALID_ARG, bad
-    for bad in (dict(ldq=260), dict(out=TWO + 2), dict(heads=258, ldq=1 << 16, ldo=1 << 16), dict(n=4097)):
+    for bad in (dict(ldq=260), dict(out=TWO + 2), dict(heads=258, ldq=1 << 16, ldo=1 << 16), dict(n=4097),
+                dict(n_rows=(1 << 22) + 1)):
         assert attend(**bad) == lq.LQ_ERR_UNSUPPORTED, bad
     assert attend(ws_bytes=64) == lq.LQ_ERR_WORKSPACE
     assert attend(n_rows=0, q=None, out=None) == lq.LQ_OK

@@ -213,6 +213,8 @@ ATTENTION = [
     (8, 4, 64, 16, [(i % 37, 1) for i in range(300)], 1),        # more units than workgroups: a unit per wave; more spans than threads
     (4, 2, 128, 16, [(i * 7 % 90, 1) for i in range(450)], 1),
     (2, 1, 64, 16, [(i % 5, 1) for i in range(1100)], 1),        # more spans than are kept
+    (1, 1, 64, 16, [(i % 2, 1) for i in range(4096)], 1),        # as many spans as a call takes
+    (1, 1, 128, 16, [(i % 2, 1) for i in range(4096)], 60),      # (with four tiles)
     (4, 2, 128, 16, [(5000, 3), (2500, 1), (1, 2)], 3),          # pages beyond a wave's first 64, chunks in byte counters
     (8, 2, 128, 64, [(3000, 1), (3100, 1)] + [(900, 1)] * 10, 1),   # chunks in four-bit counters
     (6, 1, 128, 32, [(4000, 5), (10, 5)], 5),                    # a draft split
@@ -302,6 +304,38 @@ def test_what_a_row_does_not_see_leaves_no_trace(max_rows):
         with np.errstate(invalid="ignore"):
             want = cm.attention(f64(q[a:b]).reshape(-1, heads, d), K[slots[s]], V[slots[s]], first[s], d ** -0.5, usable)
         assert_attention(f64(out[a:b]).reshape(-1, heads, d), *[np.nan_to_num(x) if i else x for i, x in enumerate(want)], 60)
+
+
+@pytest.mark.parametrize("heads,H,d,n", [(4, 2, 64, 1), (4, 2, 128, 1), (8, 2, 128, 6), (4, 4, 64, 150), (4, 2, 128, 150)])
+def test_rows_of_q_that_are_not_finite(heads, H, d, n):
+    """NaN where a row's query head holds a NaN or an infinity (also where all its scores are minus infinity), the others as if it were not there."""
+    rng = np.random.default_rng(n)
+    cache = make_cache(rng, [200], H, d, 32)
+    k, v = bf16(rng, (200, H * d)), bf16(rng, (200, H * d))
+    k[:, 0] = k[:, 0].abs() + 1                                      # first key head, column 0: positive everywhere
+    store(cache, k.cuda(), v.cuda(), None, ints([0, 200]), ints([0]))
+    q = bf16(rng, (n, heads * d)).cuda()
+    good = attend(cache, q, None, ints([0, n]), ints([200 - n]), n)
+    for i, (col, value) in enumerate([(0, -float("inf")), (0, float("inf")), (d + 3, float("nan")), (heads * d - 1, float("inf"))]):
+        bad = q.clone()
+        row = (i * 7) % n
+        bad[row, col] = value
+        out = attend(cache, bad, None, ints([0, n]), ints([200 - n]), n)
+        want = good.clone()
+        want[row, col // d * d:(col // d + 1) * d] = float("nan")
+        assert torch.equal(out.isnan(), want.isnan())
+        assert torch.equal(torch.nan_to_num(out), torch.nan_to_num(want))
+
+
+def test_a_cache_of_another_device_is_refused():
+    cache = make_cache(np.random.default_rng(0), [5], 1, 64, 16)
+    cache.device_index += 1                                          # as if its tensors lay there
+    q = torch.zeros(1, 64, dtype=torch.bfloat16, device="cuda")
+    ws = ws_for(cache)
+    with pytest.raises(ValueError, match="current device"):
+        lq.lora_cache_attention(q, torch.zeros_like(q), cache, 0, None, ints([0, 1]), ints([4]), 1, ws)
+    with pytest.raises(ValueError, match="current device"):
+        lq.lora_cache_free(cache, ints([0]), ws)
 
 
 @pytest.mark.parametrize("max_rows", [1, 20])
