@@ -420,10 +420,13 @@ __device__ __forceinline__ int block_sum(int v, int* slot)
     for (int w = 0; w < WAVES; ++w) s += slot[w];
     return s;
 }
-// inclusive prefix sum over the workgroup; total: the whole sum
+// inclusive prefix sum over the workgroup; total: the whole sum.  What would pass kScanCap, summed over the waves before, stays there: 1024
+// requests of all pages each do not fit 32 bits.
+constexpr int kScanCap = 2 * kMaxPages;
 template <int WAVES>
 __device__ __forceinline__ int block_scan(int v, int* slot, int* total)
 {
+    static_assert((long long)kWave * (kMaxPages + 1) + 2 * (long long)kScanCap < 1ll << 31, "a wave's sum behind capped ones fits");
     const int inc = wave_inclusive_scan(v);
     __syncthreads();
     if (lane_id() == kWave - 1) slot[threadIdx.x / kWave] = inc;
@@ -431,8 +434,8 @@ __device__ __forceinline__ int block_scan(int v, int* slot, int* total)
     int before = 0, all = 0;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
-        if (w < (int)threadIdx.x / kWave) before += slot[w];
-        all += slot[w];
+        if (w < (int)threadIdx.x / kWave) before = min(before + slot[w], kScanCap);
+        all = min(all + slot[w], kScanCap);
     }
     *total = all;
     return inc + before;

@@ -462,6 +462,24 @@ def test_pages_run_out_and_come_back():
     assert cache.refs.tolist() == [1] * 5 and cache.table[2, :2].tolist() == [0, 1] and cache.table[3, 0].item() == 2
 
 
+@pytest.mark.parametrize("n_pages", [(1 << 21) + 5, 4000])
+def test_requests_for_more_pages_than_32_bits_count(n_pages):
+    """1024 requests, each of all pages: the ones before the first of them are served, and nothing else is touched."""
+    n, T = 1024, 16
+    dev = dict(dtype=torch.int32, device="cuda")
+    cache = lq.PagedCache(1, 64, T, [], torch.full((n, n_pages), -1, **dev), torch.zeros(n, **dev), torch.zeros(n_pages, **dev))
+    add = torch.full((n,), n_pages * T, **dev)
+    add[0], add[1] = 3 * T, 0
+    ws = ws_for(cache, n)
+    lq.lora_cache_reserve(cache, torch.arange(n, **dev), add, ws)
+    assert lq.device_error_word(ws) == lq.LQ_DEVICE_ERR_NO_PAGES
+    assert cache.lens.sum().item() == cache.lens[0].item() == 3 * T
+    assert cache.refs.sum().item() == cache.refs[:3].sum().item() == 3
+    assert cache.table[0, :3].tolist() == [0, 1, 2]
+    cache.table[0, :3] = -1
+    assert cache.table.max().item() == -1
+
+
 def test_page_calls_with_unusable_tables():
     """Lengths and page numbers that nothing of the library wrote: reported, nothing out of range touched."""
     cache = lq.PagedCache.empty(1, 1, 64, 16, 6, 4, 3)
