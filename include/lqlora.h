@@ -346,7 +346,7 @@ lq_status lora_concat_rows(const void* parts, int32_t d, const int32_t* perm, in
  * holds already at the cost of an exponent, and a value is exact in bf16.
  *
  * head_dim 64 or 128, page_tokens 16, 32, 64, 128 or 256, n_kv_heads up to LQ_CACHE_MAX_HEADS, up to 2^22
- * pages, max_pages * page_tokens up to 2^30 (else LQ_ERR_UNSUPPORTED).
+ * pages, slots and entries of a call's lists, max_pages * page_tokens up to 2^30 (else LQ_ERR_UNSUPPORTED).
  * host_cache is read during the call and not kept.  Every call takes a workspace of at least LQ_CACHE_MIN_WORKSPACE bytes,
  * of which the first 4096 must be ZERO before the first call that uses it (as for the forward, whose workspace may
  * serve here and the other way round); word 0 is the error word.  Bit 0: a table entry, slot, page or range that cannot be
@@ -405,7 +405,8 @@ lq_status lora_cache_compact(const lq_cache* host_cache, void* const* pools, int
  * the block's new finite elements, within [-100, 119], and not below the block's exponent if the block holds positions before the
  * span's first (their codes are then brought to the new exponent); code = x * 2^-e rounded to nearest even e4m3, at most
  * +-448; NaN and infinities become NaN.  Sequences are stored in order: what a block held behind the span's last row is lost.
- * Only pages with refs == 1 are stored to (bit 0 otherwise); a slot may not be in two spans of a call. */
+ * Only pages with refs == 1 are stored to (bit 0 otherwise); a slot may not be in two spans of a call.
+ * (n_rows / 16 + 2 n_seqs) * n_kv_heads up to 2^25, here and for lora_cache_load_rows. */
 lq_status lora_cache_store_rows(const void* k, int64_t ldk, const void* v, int64_t ldv, int32_t n_rows, const lq_cache* host_cache,
                                 void* pages, const int32_t* slots, const int32_t* row_starts, const int32_t* first, int32_t n_seqs,
                                 void* workspace, size_t workspace_bytes, void* stream);

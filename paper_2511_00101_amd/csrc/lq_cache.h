@@ -7,7 +7,7 @@ namespace lq {
 
 constexpr int kBlock = LQ_CACHE_BLOCK;
 constexpr int kErrNoPages = 4;
-constexpr int kMaxPages = 1 << 22;
+constexpr int kMaxPages = 1 << 22, kMaxSlots = 1 << 22;
 
 struct CacheView {
     int n_kv_heads, t_log2, n_pages, n_slots, max_pages;

@@ -10,7 +10,8 @@ lq_status cache_view(const lq_cache* c, void* workspace, CacheView* out)
     if (!c || !c->table || !c->lens || !c->refs) return LQ_ERR_INVALID_ARG;
     if (c->n_kv_heads <= 0 || c->n_pages <= 0 || c->n_slots <= 0 || c->max_pages <= 0) return LQ_ERR_INVALID_ARG;
     const size_t bytes = lora_cache_page_bytes(c->n_kv_heads, c->head_dim, c->page_tokens);
-    if (!bytes || (int64_t)c->max_pages * c->page_tokens > (1 << 30) || c->n_pages > kMaxPages) return LQ_ERR_UNSUPPORTED;
+    if (!bytes || (int64_t)c->max_pages * c->page_tokens > (1 << 30) || c->n_pages > kMaxPages || c->n_slots > kMaxSlots)
+        return LQ_ERR_UNSUPPORTED;
     out->n_kv_heads = c->n_kv_heads;
     out->t_log2 = __builtin_ctz((unsigned)c->page_tokens);
     out->n_pages = c->n_pages;
@@ -37,6 +38,7 @@ lq_status check_spans(const lq_cache* c, const void* pages, const int32_t* row_s
 namespace {
 
 constexpr int kMaxPageTokens = 256;
+constexpr int kMaxRowWaves = 1 << 25;           // (a launch has fewer than 2^32 threads)
 
 // =================================================================================================
 // Rows into and out of the pages.  One wave takes one block of 16 positions of one head, K and V: lane (kg = lane / 16,
@@ -858,6 +860,7 @@ lq_status page_call(const lq_cache* c, int32_t n, void* workspace, size_t worksp
     if (n < 0) return LQ_ERR_INVALID_ARG;
     const lq_status st = cache_view(c, workspace, view);
     if (st != LQ_OK) return st;
+    if (n > kMaxSlots) return LQ_ERR_UNSUPPORTED;      // (workgroups of a launch)
     if (!workspace || !aligned16(workspace) || workspace_bytes < lora_cache_workspace_bytes(c, n)) return LQ_ERR_WORKSPACE;
     return LQ_OK;
 }
@@ -896,7 +899,7 @@ lq_status move_cache_rows(void* k, int64_t ldk, void* v, int64_t ldv, int32_t n_
     if (n_rows > 0 && (!k || !v || k == v)) return LQ_ERR_INVALID_ARG;
     if ((ldk % 8) || (ldv % 8) || !aligned16(k) || !aligned16(v)) return LQ_ERR_UNSUPPORTED;
     const int64_t items = (int64_t)n_rows / kBlock + 2 * (int64_t)n_seqs;
-    if (items * host_cache->n_kv_heads > 0x7fffffff) return LQ_ERR_UNSUPPORTED;
+    if (items * host_cache->n_kv_heads > kMaxRowWaves) return LQ_ERR_UNSUPPORTED;
     if (!workspace || !aligned16(workspace) || workspace_bytes < LQ_CACHE_MIN_WORKSPACE) return LQ_ERR_WORKSPACE;
     if (n_seqs == 0 || n_rows == 0) return LQ_OK;
     const Spans sp{slots, row_starts, first, n_seqs, n_rows};

@@ -35,7 +35,8 @@ def _struct(lq, **kw):
 
 BAD_CACHES = [(dict(table=None), 1), (dict(lens=None), 1), (dict(refs=None), 1), (dict(n_kv_heads=0), 1), (dict(n_pages=0), 1),
               (dict(n_slots=-1), 1), (dict(max_pages=0), 1), (dict(head_dim=80), 2), (dict(page_tokens=24), 2),
-              (dict(n_kv_heads=300), 2), (dict(max_pages=1 << 27), 2), (dict(n_pages=(1 << 22) + 1), 2)]
+              (dict(n_kv_heads=300), 2), (dict(max_pages=1 << 27), 2), (dict(n_pages=(1 << 22) + 1), 2),
+              (dict(n_slots=(1 << 22) + 1), 2)]
 
 
 def _calls(lq, c, ws=WS, ws_bytes=1 << 30, n=0):
@@ -70,6 +71,8 @@ def test_no_cache_small_workspace_and_empty_calls(lq):
     need = lq.lib().lora_cache_workspace_bytes(ctypes.addressof(c), 100)
     assert 4096 < need < 8192
     assert lq.lib().lora_cache_workspace_bytes(None, 1) == 0
+    many = _calls(lq, c, n=(1 << 22) + 1)           # more than a launch could take
+    assert {many[k] for k in ("reserve", "fork", "free", "attention")} == {lq.LQ_ERR_UNSUPPORTED}
     assert lq.lib().lora_cache_attention_workspace_bytes(ctypes.addressof(c), 0, 1) == 0
     assert lq.lib().lora_cache_attention_workspace_bytes(ctypes.addressof(c), 2, 1) >= 4096
 
@@ -86,7 +89,8 @@ def test_row_calls_refuse_before_launching(lq):
     for bad in (dict(k=None), dict(v=None), dict(k=TWO), dict(ldk=120), dict(ldv=64), dict(n_rows=-1), dict(pages=None), dict(starts=None),
                 dict(first=None)):
         assert rows(**bad) == lq.LQ_ERR_INVALID_ARG, bad
-    for bad in (dict(ldk=132), dict(ldv=129), dict(k=ONE + 8), dict(pages=ONE + 4)):
+    for bad in (dict(ldk=132), dict(ldv=129), dict(k=ONE + 8), dict(pages=ONE + 4),
+                dict(n_rows=1 << 28), dict(n=1 << 24)):
         assert rows(**bad) == lq.LQ_ERR_UNSUPPORTED, bad
     assert rows(ws_bytes=100) == lq.LQ_ERR_WORKSPACE
     assert rows(n_rows=0, k=None, v=None) == lq.LQ_OK
