@@ -160,6 +160,7 @@ struct Attention {
         };
         float m[kAttnWaves][16 * NT], l[kAttnWaves][16 * NT];
         long long sums[kAttnWaves];
+        unsigned int tiles[kAttnWaves];
         int longest[kAttnWaves], scan[kAttnWaves][2], classes[kAttnWaves][kClasses];
         int slot[2], last;
     };
@@ -797,6 +798,7 @@ __global__ __launch_bounds__(kAttnThreads, (kResident<HD, NT>)) void attention_k
     const auto tiles_of = [&](const Span& s) { return (int)(((long long)s.n * p.group + 16 * NT - 1) / (16 * NT)); };
     long long work = 0;
     int longest = 0;
+    unsigned int all_tiles = 0;                 // (stays at 2^30)
     for (int s = (int)threadIdx.x; s < n; s += kAttnThreads) {
         const Span u = load_span(p.c, p.sp, s);
         const int keys = u.n > 0 ? u.first + u.n : 0;
@@ -806,22 +808,32 @@ __global__ __launch_bounds__(kAttnThreads, (kResident<HD, NT>)) void attention_k
         if (n <= kKeptSpans) spans[s] = u;
         work += (long long)tiles * keys;
         longest = max(longest, keys);
+        all_tiles = min(all_tiles + (unsigned)tiles, 1u << 30);
     }
 #pragma unroll
     for (int d = 1; d < kWave; d <<= 1) {
+        all_tiles = min(all_tiles + (unsigned)__shfl_xor((int)all_tiles, d, kWave), 1u << 30);
         longest = max(longest, __shfl_xor(longest, d, kWave));
         work += __shfl_xor(work, d, kWave);
     }
     if (lane_id() == 0) {
         sh.sums[threadIdx.x / kWave] = work;
         sh.longest[threadIdx.x / kWave] = longest;
+        sh.tiles[threadIdx.x / kWave] = all_tiles;
     }
     __syncthreads();
     work = 0;
+    all_tiles = 0;
 #pragma unroll
     for (int w = 0; w < kAttnWaves; ++w) {
         work += sh.sums[w];
         longest = max(longest, sh.longest[w]);
+        all_tiles = min(all_tiles + sh.tiles[w], 1u << 30);
+    }
+    // Spans that share rows (row_starts that decrease) may have more tiles than the rows there are: the sums below would not fit.
+    if (all_tiles > (unsigned)((long long)p.sp.n_rows * p.group / (16 * NT) + n)) {
+        if (threadIdx.x == 0) atomicOr(p.c.err, kErrBadSegment);
+        return;
     }
     work *= heads;
     // Tiles with more positions than the chunk length are fewer than work / length and have fewer than 2 work / length chunks in all.

@@ -365,6 +365,24 @@ def test_attention_skips_spans_that_do_not_fit():
         assert (rest == 7).all()
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("max_rows", [1, 32, 160])
+def test_spans_with_more_rows_than_there_are_do_nothing(max_rows, d):
+    """row_starts that go back and forth over the same rows: reported, no row is written, and the next call is as it should be."""
+    rng = np.random.default_rng(8)
+    cache = make_cache(rng, [400], 1, d, 16)
+    store(cache, bf16(rng, (400, d)).cuda(), bf16(rng, (400, d)).cuda(), None, ints([0, 400]), ints([0]))
+    q = bf16(rng, (400, d)).cuda()
+    ws = lq.workspace(lq.lora_cache_attention_workspace_bytes(cache, 1, max_rows))
+    n = 61
+    starts = ints([0, 400] * 31)
+    out = attend(cache, q, ints([0] * n), starts, ints([0] * n), max_rows, ws=ws, expect=1)
+    assert (out == 7).all()
+    ws[:1].zero_()
+    good = attend(cache, q, None, ints([0, 400]), ints([0]), max_rows, ws=ws)
+    assert torch.equal(good, attend(cache, q, None, ints([0, 400]), ints([0]), max_rows))
+
+
 def test_pages_behind_four_gigabytes():
     """A pool of more than 2^32 bytes with the sequence in its last pages."""
     H, d, T, n_pages = 8, 128, 256, 9000
