@@ -9,7 +9,7 @@ from __future__ import annotations
 import ctypes
 import os
 from dataclasses import dataclass
-from typing import List, Optional, Sequence
+from typing import List, Optional, Sequence, Tuple
 
 import numpy as np
 import torch
@@ -438,15 +438,25 @@ def lora_cache_attention_workspace_bytes(cache: PagedCache, n_heads: int, max_ro
 _I32, _BF16 = torch.int32, torch.bfloat16
 
 
-def _index(t: torch.Tensor, n: int) -> int:
+def _index(cache: PagedCache, t: torch.Tensor, n: int) -> int:
     assert t.dtype is _I32 and t.numel() == n and t.is_contiguous()
+    if t.get_device() != cache.device_index:
+        raise ValueError("an index tensor lies on another device than the cache")
     return t.data_ptr()
 
 
+def _workspace_args(cache: PagedCache, workspace: Optional[torch.Tensor]) -> Tuple[Optional[int], int]:
+    if workspace is None:
+        return None, 0
+    if workspace.get_device() != cache.device_index:
+        raise ValueError("the workspace lies on another device than the cache")
+    return workspace.data_ptr(), workspace.nbytes
+
+
 def _cache_stream(cache: PagedCache, stream) -> Optional[int]:
-    """The stream to launch on: the current one of the cache's device, which has to be the current device.  (Read as a raw handle: a
+    """The stream to launch on: the current one of the cache's device, which has to be the current device.  (Both read as raw handles: a
     decode step's calls are as short as what it costs to make a torch.cuda.Stream of it.)"""
-    if cache.device_index != torch.cuda.current_device():
+    if cache.device_index != torch._C._cuda_getDevice():
         raise ValueError(f"the cache lies on cuda:{cache.device_index}, the current device is cuda:{torch.cuda.current_device()}")
     return torch._C._cuda_getCurrentRawStream(cache.device_index) if stream is None else _stream(stream)
 
@@ -459,44 +469,49 @@ def _call_cache(name: str, *args) -> None:
 
 def lora_cache_reserve(cache: PagedCache, slots: torch.Tensor, add: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
     """Pages for add[i] more positions of slot slots[i]."""
-    n = slots.numel()
-    _call_cache("lora_cache_reserve", cache.ref, _index(slots, n), _index(add, n), n, workspace.data_ptr(), workspace.nbytes,
-                _cache_stream(cache, stream))
+    n, stream = slots.numel(), _cache_stream(cache, stream)
+    _call_cache("lora_cache_reserve", cache.ref, _index(cache, slots, n), _index(cache, add, n), n, *_workspace_args(cache, workspace),
+                stream)
 
 
 def lora_cache_fork(cache: PagedCache, src_slots: torch.Tensor, dst_slots: torch.Tensor, workspace: torch.Tensor,
                     keep: Optional[torch.Tensor] = None, stream=None) -> None:
     """Slots dst_slots become copies of (the first `keep` positions of) slots src_slots, in all layers."""
-    n = src_slots.numel()
-    _call_cache("lora_cache_fork", cache.ref, _index(src_slots, n), _index(dst_slots, n), None if keep is None else _index(keep, n), n,
-                cache.pools.data_ptr(), len(cache.pages), workspace.data_ptr(), workspace.nbytes, _cache_stream(cache, stream))
+    n, stream = src_slots.numel(), _cache_stream(cache, stream)
+    _call_cache("lora_cache_fork", cache.ref, _index(cache, src_slots, n), _index(cache, dst_slots, n),
+                None if keep is None else _index(cache, keep, n), n, cache.pools.data_ptr(), len(cache.pages),
+                *_workspace_args(cache, workspace), stream)
 
 
 def lora_cache_free(cache: PagedCache, slots: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
     """The slots become empty; pages that no other slot holds are free."""
-    n = slots.numel()
-    _call_cache("lora_cache_free", cache.ref, _index(slots, n), n, workspace.data_ptr(), workspace.nbytes, _cache_stream(cache, stream))
+    n, stream = slots.numel(), _cache_stream(cache, stream)
+    _call_cache("lora_cache_free", cache.ref, _index(cache, slots, n), n, *_workspace_args(cache, workspace), stream)
 
 
 def lora_cache_compact(cache: PagedCache, n_live: Optional[torch.Tensor], workspace: torch.Tensor, stream=None) -> None:
     """Live pages move to the lowest numbers; n_live int32[1] (or None) receives how many there are."""
-    _call_cache("lora_cache_compact", cache.ref, cache.pools.data_ptr(), len(cache.pages), None if n_live is None else _index(n_live, 1),
-                workspace.data_ptr(), workspace.nbytes, _cache_stream(cache, stream))
+    stream = _cache_stream(cache, stream)
+    _call_cache("lora_cache_compact", cache.ref, cache.pools.data_ptr(), len(cache.pages),
+                None if n_live is None else _index(cache, n_live, 1), *_workspace_args(cache, workspace), stream)
 
 
-def _rows_matrix(t: torch.Tensor, width: int) -> int:
+def _rows_matrix(cache: PagedCache, t: torch.Tensor, width: int) -> int:
     """Leading dimension of a bf16 row matrix."""
     ld, one = t.stride()
     assert t.dtype is _BF16 and one == 1 and t.shape[1] == width
+    if t.get_device() != cache.device_index:
+        raise ValueError("a matrix of rows lies on another device than the cache")
     return ld
 
 
 def _cache_rows_args(k, v, cache, layer, slots, row_starts, first, workspace, stream):
     width, n_rows, n = cache.n_kv_heads * cache.head_dim, k.shape[0], first.numel()
+    stream = _cache_stream(cache, stream)
     assert v.shape[0] == n_rows
-    return (k.data_ptr(), _rows_matrix(k, width), v.data_ptr(), _rows_matrix(v, width), n_rows, cache.ref, cache.bases[layer],
-            None if slots is None else _index(slots, n), _index(row_starts, n + 1), _index(first, n), n,
-            workspace.data_ptr(), workspace.nbytes, _cache_stream(cache, stream))
+    return (k.data_ptr(), _rows_matrix(cache, k, width), v.data_ptr(), _rows_matrix(cache, v, width), n_rows, cache.ref, cache.bases[layer],
+            None if slots is None else _index(cache, slots, n), _index(cache, row_starts, n + 1), _index(cache, first, n), n,
+            *_workspace_args(cache, workspace), stream)
 
 
 def lora_cache_store_rows(k: torch.Tensor, v: torch.Tensor, cache: PagedCache, layer: int, slots: Optional[torch.Tensor],
@@ -513,12 +528,12 @@ def lora_cache_load_rows(k: torch.Tensor, v: torch.Tensor, cache: PagedCache, la
 
 def _attention_args(q, out, cache, layer, slots, row_starts, first, max_rows, workspace, scale, stream):
     n_rows, width = q.shape
-    n = first.numel()
+    n, stream = first.numel(), _cache_stream(cache, stream)
     assert out.shape[0] == n_rows and width % cache.head_dim == 0
-    return (q.data_ptr(), _rows_matrix(q, width), out.data_ptr(), _rows_matrix(out, width), n_rows, width // cache.head_dim,
+    return (q.data_ptr(), _rows_matrix(cache, q, width), out.data_ptr(), _rows_matrix(cache, out, width), n_rows, width // cache.head_dim,
             cache.head_dim ** -0.5 if scale is None else scale, cache.ref, cache.bases[layer],
-            None if slots is None else _index(slots, n), _index(row_starts, n + 1), _index(first, n), n, max_rows,
-            workspace.data_ptr(), workspace.nbytes, _cache_stream(cache, stream))
+            None if slots is None else _index(cache, slots, n), _index(cache, row_starts, n + 1), _index(cache, first, n), n, max_rows,
+            *_workspace_args(cache, workspace), stream)
 
 
 def lora_cache_attention(q: torch.Tensor, out: torch.Tensor, cache: PagedCache, layer: int, slots: Optional[torch.Tensor],

@@ -338,6 +338,32 @@ def test_a_cache_of_another_device_is_refused():
         lq.lora_cache_free(cache, ints([0]), ws)
 
 
+def test_tensors_of_another_device_and_no_workspace_are_refused():
+    cache = make_cache(np.random.default_rng(0), [5], 1, 64, 16)
+    q = torch.zeros(1, 64, dtype=torch.bfloat16, device="cuda")
+    good = dict(q=q, out=torch.zeros_like(q), slots=ints([0]), row_starts=ints([0, 1]), first=ints([4]),
+                workspace=lq.workspace(lq.lora_cache_attention_workspace_bytes(cache, 1, 1)))
+    for name in good:
+        with pytest.raises(ValueError, match="another device"):
+            lq.lora_cache_attention(cache=cache, layer=0, max_rows=1, **{**good, name: good[name].cpu()})
+    ws = ws_for(cache)
+    for call in (lambda i, w: lq.lora_cache_reserve(cache, ints([0]), i, w), lambda i, w: lq.lora_cache_free(cache, i, w),
+                 lambda i, w: lq.lora_cache_fork(cache, ints([0]), i, w), lambda i, w: lq.lora_cache_compact(cache, i, w),
+                 lambda i, w: lq.lora_cache_store_rows(q, good["out"], cache, 0, i, good["row_starts"], good["first"], w),
+                 lambda i, w: lq.lora_cache_load_rows(q, good["out"], cache, 0, i, good["row_starts"], good["first"], w)):
+        with pytest.raises(ValueError, match="another device"):
+            call(torch.zeros(1, dtype=torch.int32), ws)
+        with pytest.raises(ValueError, match="another device"):
+            call(ints([0]), ws.cpu())
+        with pytest.raises(lq.LqError) as err:
+            call(ints([0]), None)
+        assert err.value.status == lq.LQ_ERR_WORKSPACE
+    with pytest.raises(lq.LqError) as err:
+        lq.lora_cache_attention(cache=cache, layer=0, max_rows=1, **{**good, "workspace": None})
+    assert err.value.status == lq.LQ_ERR_WORKSPACE
+    assert cache.lens.tolist() == [5, 0]
+
+
 @pytest.mark.parametrize("max_rows", [1, 20])
 def test_rows_that_see_no_usable_page_are_zero(max_rows):
     rng = np.random.default_rng(3)
@@ -623,3 +649,92 @@ def test_a_captured_step_replays():
         assert torch.equal(caches[0][0].lens, caches[1][0].lens) and torch.equal(caches[0][0].table, caches[1][0].table)
     for c, ws in caches:
         assert lq.device_error_word(ws) == 0
+
+
+def test_captured_page_calls_and_split_sequences():
+    """Every call in one graph, with sequences that several workgroups share; replays with eager work and a wait between them."""
+    rng = np.random.default_rng(21)
+    H, d, T, S = 2, 128, 16, 4
+    lens = [5000, 2500, 30]
+    twins = []
+    k0, v0 = bf16(rng, (sum(lens), H * d)).cuda(), bf16(rng, (sum(lens), H * d)).cuda()
+    for _ in range(2):
+        c = lq.PagedCache.empty(2, H, d, T, 1000, S, 400)
+        ws = ws_for(c)
+        lq.lora_cache_reserve(c, ints([2, 0, 1]), ints([30, 5000, 2500]), ws)
+        for layer in range(2):
+            lq.lora_cache_store_rows(k0, v0, c, layer, None, ints(np.concatenate([[0], np.cumsum(lens)])), ints([0, 0, 0]), ws)
+        aws = lq.workspace(lq.lora_cache_attention_workspace_bytes(c, 4 * H, 40))
+        twins.append((c, ws, aws, ints(lens)))
+    buf = [torch.zeros(42, w * d, dtype=torch.bfloat16, device="cuda") for w in (4 * H, H, H)] + [
+        torch.zeros(42, 4 * H * d, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    slots, add, starts, last, spare, cut = ints([0, 1, 2]), ints([1, 40, 1]), ints([0, 1, 41, 42]), ints([0]), ints([3]), ints([4099])
+
+    def step(c, ws, aws, first, q, k, v, out, single):
+        lq.lora_cache_reserve(c, slots, add, ws)
+        lq.lora_cache_store_rows(k, v, c, 1, slots, starts, first, ws)
+        lq.lora_cache_attention(q, out, c, 1, slots, starts, first, 40, aws)
+        lq.lora_cache_fork(c, last, spare, ws, cut)
+        lq.lora_cache_free(c, slots[1:2], ws)
+        lq.lora_cache_compact(c, None, ws)
+        lq.lora_cache_attention(q[:1], single, c, 1, spare, starts[:2], cut - 1, 1, aws)
+        lq.lora_cache_free(c, spare, ws)
+        lq.lora_cache_reserve(c, slots[1:2], first[1:2], ws)
+        first.add_(add)
+        first[1:2].sub_(40)
+
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        step(*twins[0], *buf[:4], buf[4][:1])
+    for i in range(4):
+        inputs = [bf16(rng, tuple(b.shape), 1.0 + i).cuda() for b in buf[:3]]
+        for b, x in zip(buf, inputs):
+            b.copy_(x)
+        graph.replay()
+        out, single = torch.zeros_like(buf[3]), torch.zeros_like(buf[4])
+        step(*twins[1], *inputs, out, single[:1])
+        torch.cuda.synchronize()
+        assert torch.equal(buf[3], out) and torch.equal(buf[4], single), i
+        for name in ("lens", "table", "refs"):
+            assert torch.equal(getattr(twins[0][0], name), getattr(twins[1][0], name)), (i, name)
+    for c, ws, aws, _ in twins:
+        assert lq.device_error_word(ws) == 0 and lq.device_error_word(aws) == 0
+
+
+def test_calls_on_two_streams_and_rows_of_padding():
+    """Two streams at once, each with its workspace; rows before, between and behind the spans stay as they were."""
+    rng = np.random.default_rng(22)
+    H, d, T = 2, 128, 32
+    lens = [3000, 700, 40, 1500]
+    cache = make_cache(rng, lens, H, d, T)
+    starts = ints(np.concatenate([[0], np.cumsum(lens)]))
+    rows = sum(lens)
+    store(cache, bf16(rng, (rows, H * d)).cuda(), bf16(rng, (rows, H * d)).cuda(), None, starts, ints([0] * 4))
+    calls = []
+    for max_rows in (1, 5, 100):
+        n = [max_rows, 1, min(max_rows, 40), 1]
+        first = [t - m for t, m in zip(lens, n)]
+        begin = 3 + np.concatenate([[0], np.cumsum(n)])
+        q = bf16(rng, (int(begin[-1]) + 6, 2 * H * d)).cuda()
+        calls.append((q, ints(begin), ints(first), max_rows, int(begin[-1])))
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    ws = [lq.workspace(lq.lora_cache_attention_workspace_bytes(cache, 2 * H, 100)) for _ in range(2)]
+    want = [attend(cache, q, None, begin, first, m) for q, begin, first, m, _ in calls]
+    torch.cuda.synchronize()
+    got = [[torch.full_like(c[0], 7.0) for c in calls] for _ in range(8)]
+    torch.cuda.synchronize()
+    for r in range(8):
+        with torch.cuda.stream(streams[r % 2]):
+            for (q, begin, first, m, _), out in zip(calls, got[r]):
+                lq.lora_cache_attention(q, out, cache, 0, None, begin, first, m, ws[r % 2])
+    torch.cuda.synchronize()
+    for outs in got:
+        for out, w, (_, _, _, _, end) in zip(outs, want, calls):
+            assert torch.equal(out, w) and (out[:3] == 7).all() and (out[end:] == 7).all() and out[3:end].isfinite().all()
+    k = torch.full((rows + 9, H * d), 7.0, dtype=torch.bfloat16, device="cuda")
+    v, wr = k.clone(), ws_for(cache)
+    lq.lora_cache_load_rows(k, v, cache, 0, None, starts + 4, ints([0] * 4), wr)
+    assert lq.device_error_word(wr) == 0
+    for x in (k, v):
+        assert (x[:4] == 7).all() and (x[rows + 4:] == 7).all() and x[4:rows + 4].isfinite().all()
