@@ -34,7 +34,9 @@ template <int HD, int NT> constexpr int kResident = HD == 64 ? (NT == 1 ? 4 : NT
 constexpr int kLeastChunk = 4 * kRound;
 constexpr int kAloneLongest = kLeastChunk;      // (not split, then)
 constexpr int kClasses = 5;
-constexpr int kKeptSpans = 1024;                // spans that a workgroup keeps in LDS (16 KB); of more, a unit's is read again
+// Spans that a workgroup keeps in LDS (16 bytes each; with four row tiles as many as leave room for two workgroups on a compute unit); of
+// more, a unit's is read again.
+template <int NT> constexpr int kKeptSpans = NT < 4 ? 1024 : 256;
 __host__ __device__ constexpr int span_at(int n) { return (3 * n + 1 + 3) / 4 * 4; }
 constexpr float kNone = -3e38f;                 // a maximum before anything was seen: below every score, and finite (no case of its own anywhere)
 constexpr float kLazy = 8.f;                    // log2 of how far a score may exceed the maximum that its exponentials use
@@ -145,18 +147,20 @@ struct Attention {
     static constexpr int D = HD / 16;           // O^T rows of a lane's accumulator register set; also V words of a lane and block
     static constexpr int LD = HD / 64;          // 16-byte loads of a lane for 16 keys
     static constexpr int PITCH = HD + 4;
+    static constexpr int kHalfD = 4, kHalves = D / kHalfD;
     // Few rows: the codes are read once and bound the kernel.  Every load takes whole 128-byte lines, past the caches.
     static constexpr bool kStream = NT < 4;
     // head_dim 128: a load of K takes eight whole rows (lanes m < 8 of 16 the lower halves, the others the upper ones)
     static constexpr bool kWholeRows = kStream && LD == 2;
     struct Shared {
         union {
-            float acc[kAttnWaves][16][PITCH];
+            float acc[NT < kAttnWaves ? kAttnWaves : 1][16][PITCH];
             struct {
                 u32x4 q[NT][HD / 32][kWave];    // fragments: of bf16 values; or of codes, high parts and low parts
                 uint8_t q_exp[16][4];
             };
-            f32x2 ml[256 * 16];                 // of a split tile's chunks: maxima (then factors) and sums
+            f32x2 ml[NT < kAttnWaves ? 256 * 16 : 1];    // of a split tile's chunks: maxima (then factors) and sums
+            f32x4 part[NT < kAttnWaves ? 1 : kAttnWaves][NT][kHalfD][kWave];     // every wave's sums of 64 columns, as its registers hold them
         };
         float m[kAttnWaves][16 * NT], l[kAttnWaves][16 * NT];
         long long sums[kAttnWaves];
@@ -513,6 +517,118 @@ struct Attention {
         }
     }
 
+    // whether all other chunks of the unit's tile have left their sums
+    static __device__ __forceinline__ bool last_to_arrive(const AttnParams& p, const Unit& u, Shared& sh)
+    {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            const int i = u.slot0 / 2 * u.bits, shift = i % 32;
+            int* word = reinterpret_cast<int*>(p.arrivals) + i / 32;
+            const int old = __hip_atomic_fetch_add(word, 1 << shift, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            const bool last = ((old >> shift) & ((1 << u.bits) - 1)) == u.chunks - 1;
+            if (last) __hip_atomic_fetch_sub(word, (int)((unsigned)u.chunks << shift), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            sh.last = last;
+        }
+        __syncthreads();
+        const bool last = sh.last;
+        asm volatile("" ::: "memory");
+        return last;
+    }
+
+    // As many row tiles as waves: wave n adds up tile n, 64 columns at a time, in the layout of the accumulators (whole 1 KB accesses, also of a
+    // split tile's partial sums), and writes it from its registers.  (Maxima and sums of the rows are in LDS, behind a barrier.)  Tile after
+    // tile by all waves, with every row's columns dealt to 16 threads, took twice the barriers and read a split tile's sums one tile after
+    // the other: 8 prompts of 512 rows 61 us against 57, 64 rows behind 3000 positions 35 against 24.
+    static __device__ __forceinline__ void join_by_tiles(const AttnParams& p, const Unit& u, const Rows& tr, int wave, bool split, const State& st, Shared& sh)
+    {
+        const int lane = lane_id(), col = lane & 15, kg = lane >> 4, row = 16 * wave + col;
+        const __amdgpu_buffer_rsrc_t part = __builtin_amdgcn_make_buffer_rsrc(p.partial, 0, (int)p.partial_bytes, kRawBuffer);
+        const int slot_bytes = slot_floats<HD, NT>() * 4, stat_at = 16 * NT * HD * 4 + row * 8;
+        float a[NT], m = sh.m[0][row], l = 0.f;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            float top = sh.m[0][16 * n + col];
+#pragma unroll
+            for (int w = 1; w < kAttnWaves; ++w) top = fmaxf(top, sh.m[w][16 * n + col]);
+            a[n] = __builtin_amdgcn_exp2f(st.m[n] - top);
+        }
+#pragma unroll
+        for (int w = 1; w < kAttnWaves; ++w) m = fmaxf(m, sh.m[w][row]);
+#pragma unroll
+        for (int w = 0; w < kAttnWaves; ++w) l += sh.l[w][row] * __builtin_amdgcn_exp2f(sh.m[w][row] - m);
+        float inv = l == 0.f ? 0.f : 1.f / l;
+        const bool live = row < tr.left;
+        const int token = tr.token(row), h = u.head * p.group + tr.query(row);
+        u16* dst = p.out + (long long)(u.row0 + token) * p.ldo + h * HD + 16 * kg;
+        const auto write = [&](int half, const f32x4 (&o)[kHalfD]) {
+#pragma unroll
+            for (int i = 0; i < kHalfD; i += 4)      // 16 columns of the lane
+#pragma unroll
+                for (int r = 0; r < 4; r += 2)
+                    *reinterpret_cast<u32x4*>(dst + 16 * (half * kHalfD + i) + 4 * r) =
+                        u32x4{pack_bf16x2(o[i][r] * inv, o[i + 1][r] * inv), pack_bf16x2(o[i + 2][r] * inv, o[i + 3][r] * inv),
+                              pack_bf16x2(o[i][r + 1] * inv, o[i + 1][r + 1] * inv), pack_bf16x2(o[i + 2][r + 1] * inv, o[i + 3][r + 1] * inv)};
+        };
+#pragma unroll
+        for (int half = 0; half < kHalves; ++half) {
+            if (half) __syncthreads();
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < kHalfD; ++i) sh.part[wave][n][i][lane] = st.o[n][half * kHalfD + i] * a[n];
+            __syncthreads();
+            f32x4 o[kHalfD];
+#pragma unroll
+            for (int i = 0; i < kHalfD; ++i) {
+                o[i] = sh.part[0][wave][i][lane];
+#pragma unroll
+                for (int w = 1; w < kAttnWaves; ++w) o[i] += sh.part[w][wave][i][lane];
+            }
+            if (!split) {
+                if (live) write(half, o);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kHalfD; ++i)
+                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o[i]), part, ((wave * D + half * kHalfD + i) * kWave + lane) * 16,
+                                                           (u.slot0 + u.chunk) * slot_bytes, kSc1);
+            }
+        }
+        if (!split) return;
+        if (kg == 0) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, f32x2{m, l}), part, stat_at, (u.slot0 + u.chunk) * slot_bytes, kSc1);
+        if (!last_to_arrive(p, u, sh)) return;
+        if (16 * wave >= tr.left) return;
+        const auto stat = [&](int k) { return __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(part, stat_at, (u.slot0 + k) * slot_bytes, kSc1)); };
+        m = kNone;
+#pragma unroll 4
+        for (int k = 0; k < u.chunks; ++k) m = fmaxf(m, stat(k).x);
+        l = 0.f;
+        f32x4 o[D];
+#pragma unroll
+        for (int i = 0; i < D; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 2
+        for (int k = 0; k < u.chunks; ++k) {
+            const f32x2 ml = stat(k);
+            f32x4 v[D];
+#pragma unroll
+            for (int i = 0; i < D; ++i)
+                v[i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(part, ((wave * D + i) * kWave + lane) * 16, (u.slot0 + k) * slot_bytes, kSc1));
+            const float f = __builtin_amdgcn_exp2f(ml.x - m);
+            l += ml.y * f;
+#pragma unroll
+            for (int i = 0; i < D; ++i) o[i] += v[i] * f;
+        }
+        inv = l == 0.f ? 0.f : 1.f / l;
+        if (!live) return;
+#pragma unroll
+        for (int half = 0; half < kHalves; ++half) {
+            f32x4 x[kHalfD];
+#pragma unroll
+            for (int i = 0; i < kHalfD; ++i) x[i] = o[half * kHalfD + i];
+            write(half, x);
+        }
+    }
+
     // ALONE: the wave has the unit to itself (no other wave of the workgroup may be waited for)
     template <bool ALONE>
     static __device__ __forceinline__ void run_unit(const AttnParams& p, const Unit& u, int chunk_len, Shared& sh)
@@ -641,6 +757,10 @@ struct Attention {
         }
         __syncthreads();
         const bool split = u.chunks > 1;
+        if constexpr (NT == kAttnWaves) {
+            join_by_tiles(p, u, tr, wave, split, st, sh);
+            return;
+        }
         const int out_row = (int)threadIdx.x / 16, out_col = (int)threadIdx.x % 16 * D;
         const __amdgpu_buffer_rsrc_t part = __builtin_amdgcn_make_buffer_rsrc(p.partial, 0, (int)p.partial_bytes, kRawBuffer);
         const int slot_bytes = slot_floats<HD, NT>() * 4, stat_at = 16 * NT * HD * 4;
@@ -695,19 +815,7 @@ struct Attention {
         if (!split) return;
 
         // the last chunk of the tile adds them up
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            const int i = u.slot0 / 2 * u.bits, shift = i % 32;
-            int* word = reinterpret_cast<int*>(p.arrivals) + i / 32;
-            const int old = __hip_atomic_fetch_add(word, 1 << shift, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            const bool last = ((old >> shift) & ((1 << u.bits) - 1)) == u.chunks - 1;
-            if (last) __hip_atomic_fetch_sub(word, (int)((unsigned)u.chunks << shift), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            sh.last = last;
-        }
-        __syncthreads();
-        if (!sh.last) return;
-        asm volatile("" ::: "memory");
+        if (!last_to_arrive(p, u, sh)) return;
         for (int n = 0; n < NT; ++n) {
             const int live = min(rows - row_base - 16 * n, 16);                   // rows of this tile of 16, and the power of two above
             if (live <= 0) break;
@@ -805,7 +913,7 @@ __global__ __launch_bounds__(kAttnThreads, (kResident<HD, NT>)) void attention_k
         const int tiles = u.n > 0 ? tiles_of(u) : 0;
         units[s] = tiles;
         slots[s] = keys;
-        if (n <= kKeptSpans) spans[s] = u;
+        if (n <= kKeptSpans<NT>) spans[s] = u;
         work += (long long)tiles * keys;
         longest = max(longest, keys);
         all_tiles = min(all_tiles + (unsigned)tiles, 1u << 30);
@@ -909,7 +1017,7 @@ __global__ __launch_bounds__(kAttnThreads, (kResident<HD, NT>)) void attention_k
         const int v = id / heads;
         u.head = id - v * heads;
         const int at = uniform(last_not_above(n, v, [&](int k) { return units[k]; })), s = uniform(order[at]);
-        const Span span = n <= kKeptSpans ? spans[s] : load_span(p.c, p.sp, s);
+        const Span span = n <= kKeptSpans<NT> ? spans[s] : load_span(p.c, p.sp, s);
         u.slot = uniform(span.slot);
         u.row0 = uniform(span.row0);
         u.n = uniform(span.n);
@@ -932,7 +1040,8 @@ __global__ __launch_bounds__(kAttnThreads, (kResident<HD, NT>)) void attention_k
     });
 }
 
-size_t prefix_bytes(int n_seqs) { return (size_t)span_at(n_seqs) * sizeof(int) + (n_seqs <= kKeptSpans ? (size_t)n_seqs * sizeof(Span) : 0); }
+template <int NT>
+size_t prefix_bytes(int n_seqs) { return (size_t)span_at(n_seqs) * sizeof(int) + (n_seqs <= kKeptSpans<NT> ? (size_t)n_seqs * sizeof(Span) : 0); }
 
 template <int HD, int NT>
 hipError_t launch_attention(AttnParams p, int max_units, void* workspace, hipStream_t stream)
@@ -942,7 +1051,7 @@ hipError_t launch_attention(AttnParams p, int max_units, void* workspace, hipStr
         int dev = 0, n = 0;
         if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) n = 256;
         (void)hipFuncSetAttribute(reinterpret_cast<const void*>(attention_kernel<HD, NT>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                  (int)(prefix_bytes(LQ_CACHE_MAX_SEQS) > prefix_bytes(kKeptSpans) ? prefix_bytes(LQ_CACHE_MAX_SEQS) : prefix_bytes(kKeptSpans)));
+                                  (int)(prefix_bytes<NT>(LQ_CACHE_MAX_SEQS) > prefix_bytes<NT>(kKeptSpans<NT>) ? prefix_bytes<NT>(LQ_CACHE_MAX_SEQS) : prefix_bytes<NT>(kKeptSpans<NT>)));
         return n;
     });
     const int grid = min(max_units, n_cu * kResident<HD, NT>);
@@ -950,7 +1059,7 @@ hipError_t launch_attention(AttnParams p, int max_units, void* workspace, hipStr
     p.partial_bytes = (unsigned)kSlots<NT> * slot_floats<HD, NT>() * 4;
     p.tickets = static_cast<int*>(workspace) + 4;
     p.arrivals = static_cast<uint8_t*>(workspace) + 4 * kArrivals;
-    hipLaunchKernelGGL((attention_kernel<HD, NT>), dim3(grid), dim3(kAttnThreads), prefix_bytes(p.sp.n_seqs), stream, p);
+    hipLaunchKernelGGL((attention_kernel<HD, NT>), dim3(grid), dim3(kAttnThreads), prefix_bytes<NT>(p.sp.n_seqs), stream, p);
     return hipGetLastError();
 }
 
