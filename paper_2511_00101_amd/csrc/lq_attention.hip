@@ -11,7 +11,7 @@
 // through LDS.  The four waves of a workgroup take alternate 32-key steps with maxima of their own and are added at the end.
 //
 // Work: units of (span, row tile, key head, chunk of positions).  Every workgroup works the unit list out from the spans (a prefix
-// sum), so no plan is launched or kept; the chunk length is the batch's total work over the partial sums' slots, so that long
+// sum), so no plan is launched or kept; the chunk length is a workgroup's share of the batch's total work, so that long
 // sequences are split where there are few rows and not where there are many.  The last chunk of a tile to arrive adds the tile's
 // partial sums in chunk order.
 #include "lq_cache.h"
@@ -32,6 +32,9 @@ template <int NT> constexpr int kSlots = NT <= 2 ? 4 * kArrivalBytes : 2 * kArri
 constexpr int kManyChunksSlots = 2 * kArrivalBytes;    // with counters of eight bits
 template <int HD, int NT> constexpr int kResident = HD == 64 ? (NT == 1 ? 4 : NT == 2 ? 3 : 2) : NT == 1 ? 3 : 2;   // workgroups of a CU
 constexpr int kLeastChunk = 4 * kRound;
+// Positions that take as long as the stores, arrivals and sums of a split (30 drafts of 8 rows behind 1500 positions: 31 us in two
+// chunks each, 25 in one).
+template <int NT> constexpr int kSplitCost = NT == 1 ? 4 * kRound : 8 * kRound;
 constexpr int kAloneLongest = kLeastChunk;      // (not split, then)
 constexpr int kClasses = 5;
 // Spans that a workgroup keeps in LDS (16 bytes each; with four row tiles as many as leave room for two workgroups on a compute unit); of
@@ -948,8 +951,12 @@ __global__ __launch_bounds__(kAttnThreads, (kResident<HD, NT>)) void attention_k
     const auto length = [&](int n_slots, int most) { return max((work + n_slots / 2 - 1) / (n_slots / 2), (long long)((longest + most - 1) / most)); };
     const long long few = length(kSlots<NT>, 15), many = length(kManyChunksSlots, 255);
     const int bits = uniform(few <= many ? 4 : 8);
-    const long long round = work * (NT >= 4 ? 3 : 2) / (int)gridDim.x + 1;   // a third, half a unit per workgroup
-    const long long len = max(max(min(few, many), round), (long long)kLeastChunk);
+    // A tile has half a chunk more than its share of the work on average, so this is the length with which every workgroup gets a unit; with
+    // more than half as many tiles as workgroups, half a unit.  Nothing is split that is not longer by kSplitCost.
+    const int grid = (int)gridDim.x;
+    const long long share = work / (grid - (int)min((long long)all_tiles * heads, (long long)grid) / 2) + 1;
+    const long long split = max(max(min(few, many), share), (long long)kLeastChunk);
+    const long long len = longest <= split + kSplitCost<NT> ? max((long long)longest, split) : split;
     const int chunk_len = uniform((int)min((len + kRound - 1) / kRound * kRound, 1ll << 30));
 
     // Prefix sums, 256 spans a round; within a round the longest spans first (by powers of two below the longest of all), so that the
@@ -1011,7 +1018,10 @@ __global__ __launch_bounds__(kAttnThreads, (kResident<HD, NT>)) void attention_k
     const int n_units = uniform(unit_base) * heads;
     const bool alone = A::kAlone && uniform(longest) <= kAloneLongest && n_units > (int)gridDim.x;
     for_each_unit(p.tickets, alone ? (n_units + kAttnWaves - 1) / kAttnWaves : n_units, sh.slot, [&](int group, int) {
-        const int id = alone ? group * kAttnWaves + uniform((int)threadIdx.x / kWave) : group;
+        // Where every workgroup has one unit or two, the workgroups with the longest first unit have no second.
+        const int id = alone                                                     ? group * kAttnWaves + uniform((int)threadIdx.x / kWave)
+                       : group < grid && n_units > grid && n_units <= 2 * grid ? grid - 1 - group
+                                                                                 : group;
         if (id >= n_units) return;
         Unit u;
         const int v = id / heads;
@@ -1025,6 +1035,8 @@ __global__ __launch_bounds__(kAttnThreads, (kResident<HD, NT>)) void attention_k
         if (u.n <= 0) return;
         u.chunks = max((u.first + u.n + chunk_len - 1) / chunk_len, 1);
         u.bits = bits;
+        // (the chunks of a tile equally long)
+        const int equal = ((u.first + u.n + u.chunks - 1) / u.chunks + kRound - 1) / kRound * kRound;
         const int local = v - uniform(units[at]);
         const int back = local / u.chunks;
         u.chunk = local - back * u.chunks;
@@ -1032,11 +1044,11 @@ __global__ __launch_bounds__(kAttnThreads, (kResident<HD, NT>)) void attention_k
         u.slot0 = ((uniform(slots[at]) + back * u.chunks) * heads + u.head * u.chunks);
         if constexpr (A::kAlone) {
             if (alone) {
-                A::template run_unit<true>(p, u, chunk_len, sh);
+                A::template run_unit<true>(p, u, equal, sh);
                 return;
             }
         }
-        A::template run_unit<false>(p, u, chunk_len, sh);
+        A::template run_unit<false>(p, u, equal, sh);
     });
 }
 
