@@ -162,7 +162,7 @@ struct Attention {
                 u32x4 q[NT][HD / 32][kWave];    // fragments: of bf16 values; or of codes, high parts and low parts
                 uint8_t q_exp[16][4];
             };
-            f32x2 ml[NT < kAttnWaves ? 256 * 16 : 1];    // of a split tile's chunks: maxima (then factors) and sums
+            float sums_of_groups[NT < kAttnWaves ? NT * kAttnThreads * (D + 2) : 1];    // of a split tile's rows
             f32x4 part[NT < kAttnWaves ? 1 : kAttnWaves][NT][kHalfD][kWave];     // every wave's sums of 64 columns, as its registers hold them
         };
         float m[kAttnWaves][16 * NT], l[kAttnWaves][16 * NT];
@@ -520,6 +520,19 @@ struct Attention {
         }
     }
 
+    // Sums of D columns of a row over some of its positions, the maximum that they were taken with, and the exponentials' sum.
+    struct Sums {
+        float m = kNone, l = 0.f, o[D] = {};
+        __device__ __forceinline__ void add(const Sums& x)
+        {
+            const float top = fmaxf(m, x.m), a = __builtin_amdgcn_exp2f(m - top), b = __builtin_amdgcn_exp2f(x.m - top);
+            m = top;
+            l = l * a + x.l * b;
+#pragma unroll
+            for (int i = 0; i < D; ++i) o[i] = o[i] * a + x.o[i] * b;
+        }
+    };
+
     // whether all other chunks of the unit's tile have left their sums
     static __device__ __forceinline__ bool last_to_arrive(const AttnParams& p, const Unit& u, Shared& sh)
     {
@@ -819,64 +832,45 @@ struct Attention {
 
         // the last chunk of the tile adds them up
         if (!last_to_arrive(p, u, sh)) return;
-        for (int n = 0; n < NT; ++n) {
-            const int live = min(rows - row_base - 16 * n, 16);                   // rows of this tile of 16, and the power of two above
-            if (live <= 0) break;
-            const int row_log2 = live <= 1 ? 0 : 32 - __builtin_clz(live - 1), mask = (1 << row_log2) - 1;
-            const auto row_bytes = [&](int row) { return (16 * n + row) * HD * 4; };
-            __syncthreads();
-            for (int i = (int)threadIdx.x; i < u.chunks << row_log2; i += kAttnThreads)
-                if ((i & mask) < live)
-                    sh.ml[i] = __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(part, stat_at + (16 * n + (i & mask)) * 8 + (u.slot0 + (i >> row_log2)) * slot_bytes, 0, kSc1));
-            __syncthreads();
-            // sixteen threads a row: its maximum, its sum, and every chunk's factor
-            const int row = (int)threadIdx.x / 16, j = (int)threadIdx.x % 16;
-            if (row < live) {
-                float top = kNone, l = 0.f;
-                for (int k = j; k < u.chunks; k += 16) top = fmaxf(top, sh.ml[(k << row_log2) + row].x);
-#pragma unroll
-                for (int d = 1; d < 16; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, kWave));
-                for (int k = j; k < u.chunks; k += 16) {
-                    f32x2& ml = sh.ml[(k << row_log2) + row];
-                    const float a = __builtin_amdgcn_exp2f(ml.x - top);
-                    l += ml.y * a;
-                    ml.x = a;
-                }
-#pragma unroll
-                for (int d = 1; d < 16; d <<= 1) l += __shfl_xor(l, d, kWave);
-                if (j == 0) sh.l[0][row] = l;
-            }
-            __syncthreads();
-            // the chunks dealt to as many groups of threads as the rows leave; then the groups' sums in order
-            const int r = row & mask, group = row >> row_log2, groups = 16 >> row_log2;
-            float o[D];
-#pragma unroll
-            for (int i = 0; i < D; ++i) o[i] = 0.f;
-            if (r < live) {
+        // Sixteen threads a row, and of few rows as many groups of threads as fit, to which the chunks are dealt: a chunk's sums and its maximum come
+        // in one round trip and are added to what the group has; then the groups' sums in order.
+        const int left = rows - row_base, live = min(left, 16);
+        const int row_log2 = live <= 1 ? 0 : 32 - __builtin_clz(live - 1);       // the power of two above
+        const int r = out_row & ((1 << row_log2) - 1), group = out_row >> row_log2, groups = 16 >> row_log2;
+        Sums own[NT];
+        if (r < live) {
 #pragma unroll 2
-                for (int k = group; k < u.chunks; k += groups) {
-                    const int at = (u.slot0 + k) * slot_bytes + row_bytes(r);
-                    const float a = sh.ml[(k << row_log2) + r].x;
+            for (int k = group; k < u.chunks; k += groups)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const int row = min(16 * n + r, left - 1), at = (u.slot0 + k) * slot_bytes;
+                    Sums x;
+                    const f32x2 ml = __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(part, at + stat_at + row * 8, 0, kSc1));
+                    x.m = ml.x;
+                    x.l = ml.y;
 #pragma unroll
                     for (int i = 0; i < D; i += 4) {
-                        const f32x4 v = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(part, at + (out_col + i) * 4, 0, kSc1));
+                        const f32x4 v = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(part, at + (row * HD + out_col + i) * 4, 0, kSc1));
 #pragma unroll
-                        for (int x = 0; x < 4; ++x) o[i + x] += v[x] * a;
+                        for (int c = 0; c < 4; ++c) x.o[i + c] = v[c];
                     }
+                    own[n].add(x);
                 }
-            }
-            __syncthreads();
-            float* sums = &sh.acc[0][0][0];
+        }
+        Sums* all = reinterpret_cast<Sums*>(sh.sums_of_groups);
 #pragma unroll
-            for (int i = 0; i < D; i += 4) *reinterpret_cast<f32x4*>(sums + (int)threadIdx.x * D + i) = f32x4{o[i], o[i + 1], o[i + 2], o[i + 3]};
-            __syncthreads();
-            if (group == 0 && r < live) {
-                for (int g = 1; g < groups; ++g)
+        for (int n = 0; n < NT; ++n) all[n * kAttnThreads + (int)threadIdx.x] = own[n];
+        __syncthreads();
+        if (group == 0 && r < live) {
+            for (int g = 1; g < groups; ++g)
 #pragma unroll
-                    for (int i = 0; i < D; ++i) o[i] += sums[((((g << row_log2) + r) * 16) + j) * D + i];
+                for (int n = 0; n < NT; ++n) own[n].add(all[n * kAttnThreads + (int)threadIdx.x + (g << row_log2) * 16]);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                if (16 * n + r >= left) continue;
                 int token, h;
                 row_of(16 * n + r, token, h);
-                write_out(p, u.row0 + token, h, out_col, o, sh.l[0][r]);
+                write_out(p, u.row0 + token, h, out_col, own[n].o, own[n].l);
             }
         }
     }
