@@ -1011,6 +1011,9 @@ __global__ __launch_bounds__(kAttnThreads, (kResident<HD, NT>)) void attention_k
     // by four, and nothing is exchanged.)
     const int n_units = uniform(unit_base) * heads;
     const bool alone = A::kAlone && uniform(longest) <= kAloneLongest && n_units > (int)gridDim.x;
+    // Prompts: a key head's units in one XCD, where the heads fall evenly on them (32 of 512 rows behind 2560 positions, 8 key heads: 786 us
+    // with one counter, 756 so; 4 of 3000 rows, 5 key heads: 115 and 117).
+    const bool by_heads = NT >= 4 && (heads % 8 == 0 || 8 % heads == 0) && gridDim.x % 8 == 0;
     for_each_unit(p.tickets, alone ? (n_units + kAttnWaves - 1) / kAttnWaves : n_units, sh.slot, [&](int group, int) {
         // Where every workgroup has one unit or two, the workgroups with the longest first unit have no second.
         const int id = alone                                                     ? group * kAttnWaves + uniform((int)threadIdx.x / kWave)
@@ -1043,7 +1046,7 @@ __global__ __launch_bounds__(kAttnThreads, (kResident<HD, NT>)) void attention_k
             }
         }
         A::template run_unit<false>(p, u, equal, sh);
-    });
+    }, 0, by_heads ? 8 : 1);
 }
 
 template <int NT>

@@ -96,8 +96,10 @@ constexpr int kWaves = kThreads / kWave;
 // per unit, which also separates the units' uses of the LDS.
 //   ctr[0] draws so far, ctr[1] workgroups that left; slot: two ints of LDS
 //   it0 = 1: the workgroup's first unit has been run already; start with the second
+//   queues = 8 (of a grid that is a multiple of it): a workgroup's units are all those of one index modulo 8, later ones drawn from ctr[4 + index], so
+//   that what they have in common is in the L2 of one XCD
 template <class Body>
-__device__ __forceinline__ void for_each_unit(int* ctr, int n_units, int* slot, Body&& body, int it0 = 0)
+__device__ __forceinline__ void for_each_unit(int* ctr, int n_units, int* slot, Body&& body, int it0 = 0, int queues = 1)
 {
     const int grid = (int)gridDim.x;
     const bool more = n_units > grid, draws = n_units > 2 * grid;
@@ -105,7 +107,9 @@ __device__ __forceinline__ void for_each_unit(int* ctr, int n_units, int* slot, 
     for (int it = it0; id < n_units; ++it) {
         int next = id + grid;
         if (it > 0 && threadIdx.x == 0)
-            next = draws ? 2 * grid + __hip_atomic_fetch_add(ctr, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : n_units;
+            next = !draws ? n_units
+                   : queues == 1 ? 2 * grid + __hip_atomic_fetch_add(ctr, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)
+                                 : 2 * grid + (int)blockIdx.x % 8 + 8 * __hip_atomic_fetch_add(ctr + 4 + (int)blockIdx.x % 8, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         body(id, it);
         if (!more) break;
         if (threadIdx.x == 0) slot[it & 1] = next;
@@ -117,6 +121,8 @@ __device__ __forceinline__ void for_each_unit(int* ctr, int n_units, int* slot, 
         if (left == grid - 1) {
             __hip_atomic_store(ctr + 0, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             __hip_atomic_store(ctr + 1, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            if (queues != 1)
+                for (int q = 0; q < 8; ++q) __hip_atomic_store(ctr + 4 + q, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
     }
 }
