@@ -351,12 +351,12 @@ struct Attention {
     static __device__ __forceinline__ void pace()
     {
         if constexpr (kSharedQ) {
-            constexpr int PER = kCodesQ ? 2 : 1, PAIRS = NT * HD / 32 / PER;        // reads of a pair; pairs of products
-            __builtin_amdgcn_sched_group_barrier(0x100, AHEAD * PER, 0);           // LDS reads
+            constexpr int PAIRS = NT * HD / 32;                                     // pairs of products
+            __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);                  // LDS reads
 #pragma unroll
             for (int i = 0; i < PAIRS - AHEAD; ++i) {
                 __builtin_amdgcn_sched_group_barrier(0x8, 2, 0);                    // matrix products
-                __builtin_amdgcn_sched_group_barrier(0x100, PER, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
             }
             __builtin_amdgcn_sched_group_barrier(0x8, 2 * AHEAD, 0);
         }
@@ -1073,14 +1073,16 @@ hipError_t launch_attention(AttnParams p, int max_units, void* workspace, hipStr
 }
 
 // Row tiles of 16 of a unit: a group of query heads of one token, a draft, or a prompt.  Four tiles widen every code for 64 rows and
-// cost 5 us to set up and to join; up to 128 rows in all, units of two tiles are faster while they fill the chip's compute units no more
-// than three times (us, two tiles against four: 20 spans of 16 rows of 4 heads 9 against 12; one of 31 x 3 rows behind 18444 positions 29 against 44;
-// but 60 spans of 14 x 3 rows for 16 key heads, 1920 units, 33 against 25).
+// cost 3 us more to set up and to join: where units of two tiles do not fill the compute units, those are faster by that behind few
+// positions, and lose it only behind thousands (us, two tiles against four: 16 spans of 16 rows of 4 heads behind 300 positions 12.0 and
+// 15.3, behind 2000 28.2 and 29.1; one of 64 rows behind 1000 16.3 and 20.4, behind 12000 36.5 and 38.5, behind 30000 64 and 55; but 20 spans of
+// 16 rows, 320 units, behind 2000 33.5 and 30.3; 60 of 14 x 3 rows for 16 key heads, 1920 units, 37 and 26).
 int row_tiles(int group, int max_rows, int n_seqs, int kv_heads)
 {
     const long long rows = (long long)group * max_rows;
     if (rows <= 16) return 1;
-    return rows <= 32 || (rows <= 128 && (rows + 31) / 32 * n_seqs * kv_heads <= 768) ? 2 : 4;
+    if (rows <= 32) return 2;
+    return (rows + 31) / 32 * n_seqs * kv_heads <= (rows <= 128 ? 256 : rows <= 256 ? 128 : 0) ? 2 : 4;
 }
 
 }  // namespace

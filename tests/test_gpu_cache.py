@@ -222,6 +222,22 @@ ATTENTION = [
     (8, 1, 128, 128, [(1500, 20), (2047, 1)], 20),
     (16, 1, 128, 16, [(700, 8)], 8),                             # 128 rows: four units of two tiles
     (12, 4, 64, 32, [(3, 14), (60, 13)] * 36, 14),               # few rows, many units: four tiles
+    # four tiles by a bound far above (what the rows are does not matter)
+    (4, 4, 64, 32, [(0, 16), (17, 17), (31, 33), (100, 48)], 1000),
+    (8, 2, 128, 16, [(0, 70), (33, 129), (250, 1)], 1000),
+    (6, 2, 128, 256, [(0, 5), (255, 5), (256, 3), (40, 0), (700, 4)], 1000),
+    (4, 1, 64, 16, [(2600, 40), (0, 40)], 1000),
+    (16, 1, 128, 128, [(3500, 20), (2047, 1), (9, 8)], 1000),    # two tiles and more, in chunks, with rows left over
+    (2, 2, 128, 16, [(9000, 70), (20, 3)], 1000),
+    (1, 1, 128, 16, [(20000, 1)], 1000),
+    (8, 8, 64, 16, [(i % 29, 1 + i % 9) for i in range(140)], 1000),    # units drawn, by key heads
+    (8, 8, 128, 16, [(i * 7 % 129, 1 + i % 5) for i in range(150)], 1000),
+    (5, 5, 128, 32, [(i % 40, 1 + i % 3) for i in range(230)], 1000),   # by one counter
+    (2, 2, 128, 16, [(i * 3 % 50, 1 + i % 70) for i in range(260)], 1000),  # more spans than are kept
+    # two tiles by a bound
+    (4, 4, 64, 32, [(0, 16), (17, 17), (31, 33), (100, 48)], 30),
+    (3, 1, 128, 64, [(0, 100), (1000, 65), (4000, 1)], 20),
+    (4, 2, 128, 16, [(i * 5 % 60, 1 + i % 11) for i in range(600)], 10),
 ]
 
 
