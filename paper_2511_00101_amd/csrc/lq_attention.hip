@@ -7,13 +7,23 @@
 // layout of S^T (lane: one row; registers: keys 4 kg + r of a block of 16) IS the B operand layout of O^T = V^T P^T as far as the
 // order of the keys inside the k dimension goes, which is free: P never leaves its registers.  K's codes are loaded in the A operand
 // layout directly (16 bytes = the lane's share of two k steps), V's layout in the page gives a lane four positions of a
-// column in one word.  The codes become bf16 in registers (v_cvt_scalef32: the block's scale costs nothing), so neither K nor V passes
-// through LDS.  The four waves of a workgroup take alternate 32-key steps with maxima of their own and are added at the end.
+// column in one word.  The codes become bf16 in registers (v_cvt_scalef32: the block's scale costs nothing; K's of head_dim 128 with four
+// tiles are the operand as they are, see kCodesQ), so neither K nor V passes through LDS.  The four waves of a workgroup take alternate 32-key
+// steps with maxima of their own and are added at the end.
 //
 // Work: units of (span, row tile, key head, chunk of positions).  Every workgroup works the unit list out from the spans (a prefix
 // sum), so no plan is launched or kept; the chunk length is a workgroup's share of the batch's total work, so that long
 // sequences are split where there are few rows and not where there are many.  The last chunk of a tile to arrive adds the tile's
 // partial sums in chunk order.
+//
+// Bound and measured (8 key heads of 128 for 32 query heads unless stated):
+//   256 single tokens behind up to 4096 positions  131 us, 5.6 TB/s of codes: the rate of reading
+//   3 behind up to 32768, 32 key heads             47 us, 5.1 TB/s
+//   48 drafts of 5 rows behind up to 3000, d 64    21 us for 51 MB: 4 us until the first unit, 8 of a chunk's steps (a memory latency each), 4 of joins
+//   9 of up to 777 rows behind up to 2500          75 us, 0.61 PFLOP/s: three uneven units a workgroup, 6 us outside the steps each
+//   2 of 8192 rows                                 1.01 to 1.08 ms (by card), 1.02 to 1.09 PFLOP/s where a large product reaches 1.27: the vector
+//                                                  instructions of the softmax (64 % of the SIMDs' cycles) beside the matrix ones (49 %)
+//   4 single tokens of up to 60 positions, d 64    7 us with its launch: round trips (spans, lengths, pages, codes)
 #include "lq_cache.h"
 #include "lq_internal.h"
 
@@ -52,7 +62,7 @@ struct AttnParams {
     const u16* q; long long ldq;
     u16* out; long long ldo;
     const uint8_t* pages;
-    int n_heads, group;
+    int group;
     unsigned int group_magic;   // ceil(2^20 / group): x / group = x * magic >> 20 for x below 2^20 / group
     float c_log2;               // |scale| * log2(e)
     unsigned int q_sign;        // 0x80008000 where the scale is negative
@@ -1007,10 +1017,12 @@ __global__ __launch_bounds__(kAttnThreads, (kResident<HD, NT>)) void attention_k
     if (threadIdx.x == 0) units[n] = unit_base;
     __syncthreads();
 
-    // Many short sequences: a unit per wave.  (A unit's instructions outside its steps, some 1000 a wave, are then spent by one wave and not
-    // by four, and nothing is exchanged.)
+    // Many sequences that are short, or about equally long: a unit per wave.  (A unit's instructions outside its steps, some 1000 a wave, are then
+    // spent by one wave and not by four, and nothing is exchanged: 300 requests of up to 100 positions 39 us by workgroups, 16 by waves, 256
+    // of 2000 181 and 160; but 256 of up to 2000, the longest eight times the mean of a wave, 68 and 89.)
     const int n_units = uniform(unit_base) * heads;
-    const bool alone = A::kAlone && uniform(longest) <= kAloneLongest && n_units > (int)gridDim.x;
+    const bool even = chunk_len >= longest && (long long)longest * (2 * grid) <= work;       // (a wave's share is half the longest or more)
+    const bool alone = A::kAlone && n_units > grid && uniform(even || longest <= kAloneLongest);
     // Prompts: a key head's units in one XCD, where the heads fall evenly on them (32 of 512 rows behind 2560 positions, 8 key heads: 786 us
     // with one counter, 756 so; 4 of 3000 rows, 5 key heads: 115 and 117).
     const bool by_heads = NT >= 4 && (heads % 8 == 0 || 8 % heads == 0) && gridDim.x % 8 == 0;
@@ -1125,7 +1137,6 @@ extern "C" lq_status lora_cache_attention(const void* q, int64_t ldq, void* out,
     p.out = static_cast<u16*>(out);
     p.ldo = ldo;
     p.pages = static_cast<const uint8_t*>(pages);
-    p.n_heads = n_heads;
     p.group = n_heads / kv;
     // (not zero: a masked score is -infinity times this; 1e-30 of a score is as good as none of it)
     p.c_log2 = __builtin_fmaxf(__builtin_fabsf(scale) * 1.44269504f, 1e-30f);

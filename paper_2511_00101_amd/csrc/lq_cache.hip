@@ -46,6 +46,9 @@ constexpr int kMaxRowWaves = 1 << 25;           // (a launch has fewer than 2^32
 // of the four groups is four whole rows, and a lane has the four positions that a word of V's layout takes together.
 // A span's blocks are found without a table of them: span s owns the items from row_starts[s] / 16 + 2 s on, which are enough
 // for n rows at any offset (at most (n + 14) / 16 + 1 blocks); the others have nothing to do.
+// Bound and measured (8 key heads of 128): one row each of 256 sequences is a chain of five dependent round trips, 9.0 us to store and
+// 6.7 to read back for 15 MB; 12 prompts of up to 2048 rows by bandwidth, stored in 17.4 us (60 MB, 3.4 TB/s: the quantisation's vector instructions,
+// half of its cycles, stand between a block's loads and its stores) and read back in 11.3 us (5.3 TB/s, the rate of a copy).
 // =================================================================================================
 // A wave's start is a chain of dependent round trips (spans, span, table and rows, page); nothing of a trip waits for a check of the one
 // before: indexes are brought into range instead, and what was found is looked at when all of it is there.
@@ -362,9 +365,15 @@ __global__ __launch_bounds__(256) void load_rows_kernel(CacheView c, Spans sp, c
 // which workgroups run.  First the plan: which request gets how many pages (a running sum), and which pages are free (a rank).
 // Up to kSmallPages pages one workgroup does all of it in one launch; beyond, pages are counted in segments by a workgroup each beside
 // the requests' plan, and a second launch hands out.  What the plan leaves (table rows, copies of pages) is the last launch's.
+// Bound and measured: reserve and free by latency (a few KB): 512 requests of a page each 7.6 us of 8192 pages, 9.6 of 65536 (kernels 3.3 and
+// 4.2); 400 slots freed 3.4.  A fork's and a compaction's copies by bandwidth: 132 MB of a fork in 27 us behind a plan of 5.6, 381 MB of a
+// compaction in 71 behind lists of 4.7 (4.9 and 5.4 TB/s, read and written; a large copy reaches 5.1).
 // =================================================================================================
 constexpr int kSegPages = 4096;
-constexpr int kSmallPages = 8192;       // pages up to which one workgroup does it (1024 a round)
+// Pages up to which one workgroup does it, 1024 a round, all rounds' counts requested up front (64 requests of a page each, of 40 each: with
+// 8192 pages 6.7 and 9.7 us in one launch, 7.8 and 10.9 in two; with 16000 8.3 and 11.5 against 9.0 and 11.2, and smaller pools wait
+// 0.3 us longer for the loads of the larger).
+constexpr int kSmallPages = 8192;
 constexpr int kRefGroups = 16;          // workgroups that move the counts of a compaction's pages
 constexpr int kMarkSlots = 8192;        // slots whose first mention is looked for in LDS; of more, in the workspace
 constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / kWave;

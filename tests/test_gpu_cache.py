@@ -238,6 +238,9 @@ ATTENTION = [
     (4, 4, 64, 32, [(0, 16), (17, 17), (31, 33), (100, 48)], 30),
     (3, 1, 128, 64, [(0, 100), (1000, 65), (4000, 1)], 20),
     (4, 2, 128, 16, [(i * 5 % 60, 1 + i % 11) for i in range(600)], 10),
+    # many about equally long: a unit per wave beyond the short ones
+    (8, 8, 64, 16, [(560 + i % 40, 1) for i in range(140)], 1),
+    (16, 8, 128, 64, [(600 - i % 33, 1) for i in range(105)], 1),
 ]
 
 
