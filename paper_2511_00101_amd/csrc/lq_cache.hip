@@ -46,9 +46,10 @@ constexpr int kMaxRowWaves = 1 << 25;           // (a launch has fewer than 2^32
 // of the four groups is four whole rows, and a lane has the four positions that a word of V's layout takes together.
 // A span's blocks are found without a table of them: span s owns the items from row_starts[s] / 16 + 2 s on, which are enough
 // for n rows at any offset (at most (n + 14) / 16 + 1 blocks); the others have nothing to do.
-// Bound and measured (8 key heads of 128): one row each of 256 sequences is a chain of five dependent round trips, 9.0 us to store and
-// 6.7 to read back for 15 MB; 12 prompts of up to 2048 rows by bandwidth, stored in 17.4 us (60 MB, 3.4 TB/s: the quantisation's vector instructions,
-// half of its cycles, stand between a block's loads and its stores) and read back in 11.3 us (5.3 TB/s, the rate of a copy).
+// Bound and measured (8 key heads of 128, in a graph): one row each of 256 sequences is a chain of five dependent round trips, 6.5 us to store and
+// 4.4 to read back for 15 MB; 12 prompts of up to 2048 rows by bandwidth, 12.1 and 11.8 us for 60 MB each (5.0 and 5.1 TB/s, the rate of
+// a copy).  Storing, a block's elements are looked at as packed magnitudes and converted in pairs, the scale being an operand of the conversion;
+// with the elements widened to fp32 one by one the vector instructions took half of the cycles (8.0 and 15.0 us).
 // =================================================================================================
 // A wave's start is a chain of dependent round trips (spans, span, table and rows, page); nothing of a trip waits for a check of the one
 // before: indexes are brought into range instead, and what was found is looked at when all of it is there.
@@ -144,27 +145,46 @@ __device__ __forceinline__ void store_words(uint8_t* p, const unsigned int (&w)[
 __device__ __forceinline__ bool finite(float v) { return fabsf(v) < __builtin_inff(); }
 
 // largest of the wave's values, in every lane: rotations within rows of 16 lanes, then rows and halves swapped
-__device__ __forceinline__ float wave_max(float v)
+__device__ __forceinline__ unsigned int wave_max(unsigned int v)
 {
     typedef __attribute__((ext_vector_type(2))) unsigned int pair;
-#define LQ_ROTATED(n) __uint_as_float((unsigned int)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x120 + (n), 0xf, 0xf, false))
-    v = fmaxf(v, LQ_ROTATED(1));
-    v = fmaxf(v, LQ_ROTATED(2));
-    v = fmaxf(v, LQ_ROTATED(4));
-    v = fmaxf(v, LQ_ROTATED(8));
+#define LQ_ROTATED(n) (unsigned int)__builtin_amdgcn_update_dpp(0, (int)v, 0x120 + (n), 0xf, 0xf, false)
+    v = max(v, LQ_ROTATED(1));
+    v = max(v, LQ_ROTATED(2));
+    v = max(v, LQ_ROTATED(4));
+    v = max(v, LQ_ROTATED(8));
 #undef LQ_ROTATED
-    const pair a = __builtin_bit_cast(pair, __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false));
-    v = fmaxf(__uint_as_float(a.x), __uint_as_float(a.y));
-    const pair b = __builtin_bit_cast(pair, __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false));
-    return fmaxf(__uint_as_float(b.x), __uint_as_float(b.y));
+    const pair a = __builtin_bit_cast(pair, __builtin_amdgcn_permlane16_swap(v, v, false, false));
+    v = max(a.x, a.y);
+    const pair b = __builtin_bit_cast(pair, __builtin_amdgcn_permlane32_swap(v, v, false, false));
+    return max(b.x, b.y);
+}
+
+constexpr unsigned int kBf16Inf = 0x7f80;
+typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
+// larger of each half, as unsigned numbers (of magnitudes: NaN, infinity, finite values by size)
+__device__ __forceinline__ unsigned int larger_halves(unsigned int a, unsigned int b)
+{
+    return __builtin_bit_cast(unsigned int, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+// codes of four bf16 values, finite and at most 448 * scale (a power of two)
+__device__ __forceinline__ unsigned int encode4_in_range(unsigned int w01, unsigned int w23, float scale)
+{
+    typedef __attribute__((ext_vector_type(2))) short s16x2;
+    typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+    s16x2 c = {0, 0};
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(c, __builtin_bit_cast(bf16x2, w01), scale, false);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(c, __builtin_bit_cast(bf16x2, w23), scale, true);
+    return __builtin_bit_cast(unsigned int, c);
 }
 
 // least e with amax <= 448 * 2^e (448 = 1.75 * 2^8), within [-100, 119]
+constexpr int kLargestExponent = 119;
 __device__ __forceinline__ int scale_exponent(float amax)
 {
     const unsigned int u = __float_as_uint(amax);
     const int e = (int)(u >> 23) - 127 - ((u & 0x7fffffu) <= 0x600000u ? 8 : 7);
-    return min(max(e, -100), 119);
+    return min(max(e, -100), kLargestExponent);
 }
 
 // two values, already brought to the block's scale, as two e4m3 codes in the low 16 bits
@@ -236,21 +256,36 @@ __global__ __launch_bounds__(256) void store_rows_kernel(CacheView c, Spans sp, 
         for (int t = 0; t < 4; ++t) load_words(kc + t * HD, old_k[t]);
         load_words(vc, old_v);
     }
-    float amax[2] = {0.f, 0.f};
+    unsigned int amax[2];                       // largest magnitude of the new elements, as bf16
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int x = 0; x < 2; ++x) {
+        unsigned int m = 0;
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
+        for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int d = 0; d < D; ++d) {
-                const float f = kv[x][t].at(d);
-                const bool counts = bool(is_new >> t & 1u) & finite(f);
-                amax[x] = fmaxf(amax[x], counts ? fabsf(f) : 0.f);
-            }
+            for (int i = 0; i < D / 2; ++i) m = larger_halves(m, kv[x][t].w[i] & (is_new >> t & 1u ? 0x7fff7fffu : 0u));
+        amax[x] = wave_max(max(m & 0xffffu, m >> 16));
+    }
+    bool in_range[2] = {amax[0] < kBf16Inf, amax[1] < kBf16Inf};    // wave uniform
+    if (!in_range[0] || !in_range[1]) {         // the largest of the finite ones
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            unsigned int m = 0;
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int d = 0; d < D; ++d) {
+                    const unsigned int v = kv[x][t].w[d / 2] >> (16 * (d % 2)) & 0x7fffu;
+                    m = max(m, (is_new >> t & 1u) && v < kBf16Inf ? v : 0u);
+                }
+            amax[x] = wave_max(m);
+        }
+    }
     int e[2], e_old[2];
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-        e[x] = scale_exponent(wave_max(amax[x]));
+        e[x] = scale_exponent(__uint_as_float(amax[x] << 16));
+        in_range[x] = in_range[x] && e[x] < kLargestExponent;
         e_old[x] = has_old ? (int)(old_e >> (8 * x) & 0xffu) - 127 : e[x];
         e[x] = max(e[x], e_old[x]);
     }
@@ -259,6 +294,7 @@ __global__ __launch_bounds__(256) void store_rows_kernel(CacheView c, Spans sp, 
     for (int t = 0; t < 4; ++t) is_old |= pos + t < j.first ? 1u << t : 0u;
 
     const float r[2] = {block_scale((unsigned)(127 - e[0])), block_scale((unsigned)(127 - e[1]))};
+    const float scale[2] = {block_scale((unsigned)(127 + e[0])), block_scale((unsigned)(127 + e[1]))};
     // the kept codes at the new exponents (positions behind the last row, which share a word of V with others, are nobody's)
     const bool again[2] = {has_old && e[0] != e_old[0], has_old && e[1] != e_old[1]};      // wave uniform
     if (again[0]) {
@@ -290,8 +326,12 @@ __global__ __launch_bounds__(256) void store_rows_kernel(CacheView c, Spans sp, 
         unsigned int w[W];
 #pragma unroll
         for (int i = 0; i < W; ++i) {
-            const float f[4] = {kv[0][t].at(4 * i), kv[0][t].at(4 * i + 1), kv[0][t].at(4 * i + 2), kv[0][t].at(4 * i + 3)};
-            const unsigned int code = encode4(f, r[0]);
+            unsigned int code;
+            if (in_range[0]) code = encode4_in_range(kv[0][t].w[2 * i], kv[0][t].w[2 * i + 1], scale[0]);
+            else {
+                const float f[4] = {kv[0][t].at(4 * i), kv[0][t].at(4 * i + 1), kv[0][t].at(4 * i + 2), kv[0][t].at(4 * i + 3)};
+                code = encode4(f, r[0]);
+            }
             w[i] = fresh ? code : old_k[t][i];
         }
         if (fresh || (again[0] && (is_old >> t & 1u))) store_words(kc + t * HD, w);
@@ -299,11 +339,23 @@ __global__ __launch_bounds__(256) void store_rows_kernel(CacheView c, Spans sp, 
     // V: a word holds four positions of a column
     const unsigned int sel = (is_new & 1u ? 0xffu : 0u) | (is_new & 2u ? 0xff00u : 0u) | (is_new & 4u ? 0xff0000u : 0u) | (is_new & 8u ? 0xff000000u : 0u);
     unsigned int w[D];
+    if (in_range[1]) {
 #pragma unroll
-    for (int d = 0; d < D; ++d) {
-        const float f[4] = {kv[1][0].at(d), kv[1][1].at(d), kv[1][2].at(d), kv[1][3].at(d)};
-        w[d] = (encode4(f, r[1]) & sel) | (old_v[d] & ~sel);
+        for (int d = 0; d < D; d += 2) {        // two columns: codes of two positions a word, then bytes sorted by column
+            const unsigned int low = encode4_in_range(kv[1][0].w[d / 2], kv[1][1].w[d / 2], scale[1]);
+            const unsigned int high = encode4_in_range(kv[1][2].w[d / 2], kv[1][3].w[d / 2], scale[1]);
+            w[d] = __builtin_amdgcn_perm(high, low, 0x06040200u);
+            w[d + 1] = __builtin_amdgcn_perm(high, low, 0x07050301u);
+        }
+    } else {
+#pragma unroll
+        for (int d = 0; d < D; ++d) {
+            const float f[4] = {kv[1][0].at(d), kv[1][1].at(d), kv[1][2].at(d), kv[1][3].at(d)};
+            w[d] = encode4(f, r[1]);
+        }
     }
+#pragma unroll
+    for (int d = 0; d < D; ++d) w[d] = (w[d] & sel) | (old_v[d] & ~sel);
     if (is_new || (is_old && again[1])) store_words(vc, w);
     if (lane < 2) se[lane] = (uint8_t)((lane == 0 ? e[0] : e[1]) + 127);
 }
