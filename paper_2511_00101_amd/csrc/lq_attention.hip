@@ -40,7 +40,10 @@ constexpr int kArrivalBytes = kWsHeaderBytes - 4 * kArrivals;
 // Partial-sum slots of a call: a split tile has at least two, and its counter's number is its first slot's / 2.
 template <int NT> constexpr int kSlots = NT <= 2 ? 4 * kArrivalBytes : 2 * kArrivalBytes;
 constexpr int kManyChunksSlots = 2 * kArrivalBytes;    // with counters of eight bits
-template <int HD, int NT> constexpr int kResident = HD == 64 ? (NT == 1 ? 4 : NT == 2 ? 3 : 2) : NT == 1 ? 3 : 2;   // workgroups of a CU
+// workgroups of a CU: as many as the accumulators, the codes of a step and Q leave registers for without spilling
+template <int HD, int NT> constexpr int kResident = HD == 64 ? (NT == 1 ? 4 : NT == 2 ? 3 : 2) : NT == 1 ? 3 : 2;
+// (us, half as long and twice as long beside it: 8 drafts of 8 rows behind up to 6000 positions 24.2, 21.0, 22.0; one token behind 3000 11.6, 12.8,
+// 14.5, behind 30000 25.7, 23.2, 21.8)
 constexpr int kLeastChunk = 4 * kRound;
 // Positions that take as long as the stores, arrivals and sums of a split (30 drafts of 8 rows behind 1500 positions: 31 us in two
 // chunks each, 25 in one).
@@ -161,7 +164,8 @@ struct Attention {
     static constexpr int LD = HD / 64;          // 16-byte loads of a lane for 16 keys
     static constexpr int PITCH = HD + 4;
     static constexpr int kHalfD = 4, kHalves = D / kHalfD;
-    // Few rows: the codes are read once and bound the kernel.  Every load takes whole 128-byte lines, past the caches.
+    // Few rows: the codes are read once and bound the kernel.  Every load takes whole 128-byte lines, past the caches (256 tokens behind up to
+    // 4096 positions 130 us, with plain loads 143; prompts, whose tiles read the same codes, the other way round: 1167 and 1097).
     static constexpr bool kStream = NT < 4;
     // head_dim 128: a load of K takes eight whole rows (lanes m < 8 of 16 the lower halves, the others the upper ones)
     static constexpr bool kWholeRows = kStream && LD == 2;
@@ -244,11 +248,12 @@ struct Attention {
 
     struct Scores { f32x4 s[2][NT]; };
     static constexpr bool kAlone = NT == 1;     // a unit per wave is offered
-    static constexpr bool kSharedQ = NT >= 4;   // Q's fragments in LDS (the waves have the same rows): 64 registers less
+    static constexpr bool kSharedQ = NT >= 4;   // Q's fragments in LDS (the waves have the same rows): 64 registers less, without which the sums spill
     // Prompts with head_dim 128: K's codes are the operand themselves, with their block's exponent as the matrix instruction's scale, and a row of Q
     // is two rows of codes under one exponent e: q = 2^e (high + low / 16).  A bf16 value's eight bits are a four-bit high part and a four-bit
     // remainder, so the split is exact down to 2^-22 of the row's largest element; two 16 x 16 x 128 products take what four
-    // bf16 ones take, without the conversion of K.
+    // bf16 ones take, without the conversion of K (two prompts of 8192 rows 1241 -> 1137 us).  With head_dim 64 one product of the depth 128 would
+    // hold both parts, but K's duplicated halves have to be exchanged between lanes, as many instructions as the conversion.
     static constexpr bool kCodesQ = kSharedQ && HD == 128;
     typedef __attribute__((ext_vector_type(8))) int i32x8;
     static constexpr int kAhead = 3;
