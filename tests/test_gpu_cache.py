@@ -410,6 +410,23 @@ def test_attention_skips_spans_that_do_not_fit():
         assert (rest == 7).all()
 
 
+@pytest.mark.parametrize("max_rows", [1, 32, 1000])
+def test_calls_whose_spans_are_all_empty(max_rows):
+    """Rows that belong to nobody, slots without a position: nothing is written, nothing is reported."""
+    rng = np.random.default_rng(9)
+    cache = make_cache(rng, [0, 33, 0], 2, 64, 16)
+    pages = cache.pages[0].clone()
+    slots, starts, first = ints([0, 1, 2, 0]), ints([5] * 5), ints([0, 33, 0, 0])
+    k, v = bf16(rng, (20, 128)).cuda(), bf16(rng, (20, 128)).cuda()
+    store(cache, k, v, slots, starts, first)
+    assert torch.equal(cache.pages[0], pages)
+    kept, ws = (k.clone(), v.clone()), ws_for(cache)
+    lq.lora_cache_load_rows(k, v, cache, 0, slots, starts, first, ws)
+    assert lq.device_error_word(ws) == 0 and torch.equal(k, kept[0]) and torch.equal(v, kept[1])
+    out = attend(cache, bf16(rng, (20, 256)).cuda(), slots, starts, first, max_rows)
+    assert (out == 7).all()
+
+
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("max_rows", [1, 32, 160])
 def test_spans_with_more_rows_than_there_are_do_nothing(max_rows, d):
