@@ -421,6 +421,8 @@ lq_status lora_cache_load_rows(void* k, int64_t ldk, void* v, int64_t ldv, int32
  *     out[t, h, :] = sum_j p_j V[j, h / G, :],   p = softmax_j(scale * q[t, h, :] . K[j, h / G, :]),   j = 0 .. position of t
  *   q, out   bf16 [n_rows, n_heads * head_dim], leading dimensions ldq, ldo; n_heads a multiple G of n_kv_heads, up to
  *            LQ_CACHE_MAX_HEADS; out may not overlap q.  Sums and softmax in fp32, p rounded to bf16 for the product with V.
+ *            Elements of q below 2^-31 of their head's largest (or of 2^-97, if that is more) may be off by up to 2^-39 of
+ *            it: long tiles hold q as a sum of 8-bit parts.
  *            An element of q that is not finite makes its row and head NaN (where it sees a position).  Scores lie within fp32's range.
  *   max_rows the largest number of rows of a span (a bound from above will do): picks the kernel's tile, no result depends on
  *            it but for the order of sums

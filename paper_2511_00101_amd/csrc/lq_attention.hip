@@ -169,12 +169,23 @@ struct Attention {
     static constexpr bool kStream = NT < 4;
     // head_dim 128: a load of K takes eight whole rows (lanes m < 8 of 16 the lower halves, the others the upper ones)
     static constexpr bool kWholeRows = kStream && LD == 2;
+    static constexpr bool kSharedQ = NT >= 4;   // Q's fragments in LDS (the waves have the same rows): 64 registers less, without which the sums spill
+    // Prompts with head_dim 128: K's codes are the operand themselves, with their block's exponent as the matrix instruction's scale, and Q is the sum
+    // of rows of codes: q = 2^e (high + low 2^-11 + last 2^-22), one e a row, high and last in e4m3, low in e5m2.  Of a bf16 value's
+    // eight bits high takes four and low the other three (a nearest one's remainder has a sign); where the row's largest element is more than 2^14
+    // times larger, high loses bits, and last has what low cannot hold: the sum is exact down to 2^-31 of the largest element, and off by at most
+    // 2^-39 of it below (and of 2^-97 in rows that are smaller).  Last is multiplied only for row tiles that have one (of Gaussian rows one of eleven; 1.5 % of the
+    // time of two 8192-row prompts).  Two 16 x 16 x 128 products take what four bf16 ones take, without the conversion of K (two prompts of 8192 rows 1137 us
+    // against 1241 when it was brought in).  With head_dim 64 one product of the depth 128 would hold both parts, but K's duplicated halves have to be
+    // exchanged between lanes, as many instructions as the conversion.
+    static constexpr bool kCodesQ = kSharedQ && HD == 128;
     struct Shared {
         union {
             float acc[NT < kAttnWaves ? kAttnWaves : 1][16][PITCH];
             struct {
-                u32x4 q[NT][HD / 32][kWave];    // fragments: of bf16 values; or of codes, high parts and low parts
+                u32x4 q[NT][kCodesQ ? 6 : HD / 32][kWave];      // fragments: of bf16 values; or of codes, high, low and last parts
                 uint8_t q_exp[16][4];
+                uint8_t q_last[4];              // whether the row tile has last parts that are not zero
             };
             float sums_of_groups[NT < kAttnWaves ? NT * kAttnThreads * (D + 2) : 1];    // of a split tile's rows
             f32x4 part[NT < kAttnWaves ? 1 : kAttnWaves][NT][kHalfD][kWave];     // every wave's sums of 64 columns, as its registers hold them
@@ -248,59 +259,90 @@ struct Attention {
 
     struct Scores { f32x4 s[2][NT]; };
     static constexpr bool kAlone = NT == 1;     // a unit per wave is offered
-    static constexpr bool kSharedQ = NT >= 4;   // Q's fragments in LDS (the waves have the same rows): 64 registers less, without which the sums spill
-    // Prompts with head_dim 128: K's codes are the operand themselves, with their block's exponent as the matrix instruction's scale, and a row of Q
-    // is two rows of codes under one exponent e: q = 2^e (high + low / 16).  A bf16 value's eight bits are a four-bit high part and a four-bit
-    // remainder, so the split is exact down to 2^-22 of the row's largest element; two 16 x 16 x 128 products take what four
-    // bf16 ones take, without the conversion of K (two prompts of 8192 rows 1241 -> 1137 us).  With head_dim 64 one product of the depth 128 would
-    // hold both parts, but K's duplicated halves have to be exchanged between lanes, as many instructions as the conversion.
-    static constexpr bool kCodesQ = kSharedQ && HD == 128;
     typedef __attribute__((ext_vector_type(8))) int i32x8;
     static constexpr int kAhead = 3;
+    static constexpr int kLowExp = 11, kLastExp = 22;
 
-    static __device__ __forceinline__ void split_q(const u32x4 (&w)[4], u32x4 (&high)[2], u32x4 (&low)[2], unsigned int& exponent)
+    // two values' high parts, low parts, and what those leave (times 2^kLastExp)
+    static __device__ __forceinline__ unsigned int split2(const float* x, float r, unsigned int& low, float (&left)[2])
     {
-        float x[32], amax = 0.f;
+        const float a[2] = {x[0] * r, x[1] * r};
+        const unsigned int high = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(a[0], a[1], 0, false) & 0xffffu;
+        const f32x2 back = __builtin_amdgcn_cvt_pk_f32_fp8((int)high, false);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) left[k] = (a[k] - back[k]) * (1 << kLowExp);
+        low = (unsigned)__builtin_amdgcn_cvt_pk_bf8_f32(left[0], left[1], 0, false) & 0xffffu;
+        const f32x2 low_back = __builtin_amdgcn_cvt_pk_f32_bf8((int)low, false);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) left[k] = (left[k] - low_back[k]) * (1 << (kLastExp - kLowExp));
+        return high;
+    }
+    // The row tile's fragments into LDS; w: the lane's share of its row
+    static __device__ __forceinline__ void split_q(const u32x4 (&w)[4], Shared& sh, int n)
+    {
+        const int lane = lane_id();
+        float x[32], amax = 0.f, any = 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) unpack8(w[i], x + 8 * i);
 #pragma unroll
         for (int i = 0; i < 32; ++i) amax = fmaxf(amax, fabsf(x[i]));
         amax = column_max(amax);
         const unsigned int u = __float_as_uint(fminf(amax, 3.4e38f));
-        const int e = max((int)(u >> 23) - 127 - ((u & 0x7fffffu) <= 0x600000u ? 8 : 7), -118);   // least with amax <= 448 * 2^e
+        const int e = max((int)(u >> 23) - 127 - ((u & 0x7fffffu) <= 0x600000u ? 8 : 7), kLastExp - 127);     // least with amax <= 448 * 2^e
         const float r = __uint_as_float((unsigned)(127 - e) << 23);
-        exponent = (unsigned)(e + 127);                                // E8M0, of the high parts; the low parts' is 4 less
+        if (lane < 16) sh.q_exp[lane][n] = (uint8_t)(e + 127);         // E8M0, of the high parts; the others' are kLowExp and kLastExp less
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            unsigned int hi = 0, lo = 0;
+        for (int g = 0; g < 2; ++g) {
+            u32x4 high, low;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                float a[2], rest[2];
+            for (int i = 0; i < 4; ++i) {
+                unsigned int lo[2], hi[2];
 #pragma unroll
-                for (int k = 0; k < 2; ++k) a[k] = x[4 * i + 2 * h + k] * r;
-                const unsigned int code = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(a[0], a[1], 0, false) & 0xffffu;
-                const f32x2 back = __builtin_amdgcn_cvt_pk_f32_fp8((int)code, false);
-#pragma unroll
-                for (int k = 0; k < 2; ++k) rest[k] = (a[k] - back[k]) * 16.f;
-                hi |= code << (16 * h);
-                lo |= ((unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(rest[0], rest[1], 0, false) & 0xffffu) << (16 * h);
+                for (int h = 0; h < 2; ++h) {
+                    float left[2];
+                    hi[h] = split2(x + 16 * g + 4 * i + 2 * h, r, lo[h], left);
+                    any = fmaxf(any, fmaxf(fabsf(left[0]), fabsf(left[1])));       // (a NaN's high and low parts are NaN: the last one may be anything)
+                }
+                high[i] = hi[0] | hi[1] << 16;
+                low[i] = lo[0] | lo[1] << 16;
             }
-            high[i / 4][i % 4] = hi;
-            low[i / 4][i % 4] = lo;
+            sh.q[n][g][lane] = high;
+            sh.q[n][2 + g][lane] = low;
+        }
+        const bool last = __any(any > 0.f);
+        if (lane == 0) sh.q_last[n] = last;
+        if (!last) return;
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            u32x4 part;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                unsigned int la[2], lo;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float left[2];
+                    split2(x + 16 * g + 4 * i + 2 * h, r, lo, left);
+                    la[h] = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(left[0], left[1], 0, false) & 0xffffu;
+                }
+                part[i] = la[0] | la[1] << 16;
+            }
+            sh.q[n][4 + g][lane] = part;
         }
     }
 
-    // n: the byte of qe that holds the exponents of row tile n (a constant once the loops are unrolled)
+    // n: the byte of qe that holds the exponents of row tile n (a constant once the loops are unrolled); FORMAT of b: 0 e4m3, 1 e5m2
+    template <int FORMAT>
     static __device__ __forceinline__ f32x4 mfma_codes(int n, i32x8 a, i32x8 b, f32x4 c, int ke, int qe)
     {
-        return n == 0   ? __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, ke, 0, qe)
-               : n == 1 ? __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, ke, 1, qe)
-               : n == 2 ? __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, ke, 2, qe)
-                        : __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, ke, 3, qe);
+        return n == 0   ? __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, FORMAT, 0, ke, 0, qe)
+               : n == 1 ? __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, FORMAT, 0, ke, 1, qe)
+               : n == 2 ? __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, FORMAT, 0, ke, 2, qe)
+                        : __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, FORMAT, 0, ke, 3, qe);
     }
 
-    // q_exp: with kCodesQ, the exponents of the lane's row in the row tiles, a byte each
-    static __device__ __forceinline__ void scores(const Step<HD>& s, const bf16x8 (&q)[kSharedQ ? 1 : NT][HD / 32], int q_exp, const Shared& sh, Scores& sc)
+    // with kCodesQ: q_exp the exponents of the lane's row in the row tiles, a byte each; q_last a byte of 1 for each tile with last parts
+    static __device__ __forceinline__ void scores(const Step<HD>& s, const bf16x8 (&q)[kSharedQ ? 1 : NT][HD / 32], int q_exp, int q_last, const Shared& sh,
+                                                  Scores& sc)
     {
 #pragma unroll
         for (int b = 0; b < 2; ++b)
@@ -318,11 +360,12 @@ struct Attention {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) a[b][i] = (int)k[b][i / 4][i % 4];
             const int e0 = uniform((int)s.e[0]) & 0xff, e1 = uniform((int)s.e[1]) & 0xff;
-            const int low_exp = q_exp - 0x04040404;
-            const auto fragment = [&](int i) {      // of row tile i / 2: its high parts, its low parts
-                const u32x4 x = sh.q[i / 2][i % 2 * 2][lane_id()], y = sh.q[i / 2][i % 2 * 2 + 1][lane_id()];
+            const int low_exp = q_exp - 0x01010101 * kLowExp;
+            const auto parts = [&](int n, int which) {      // of row tile n: its high parts, its low parts, its last ones
+                const u32x4 x = sh.q[n][which * 2][lane_id()], y = sh.q[n][which * 2 + 1][lane_id()];
                 return i32x8{(int)x.x, (int)x.y, (int)x.z, (int)x.w, (int)y.x, (int)y.y, (int)y.z, (int)y.w};
             };
+            const auto fragment = [&](int i) { return parts(i / 2, i % 2); };
             // kAhead fragments on their way while a pair of products runs (in this order: left to the scheduler, the reads are either all in
             // front, which takes registers that spill, or each is waited for)
             i32x8 f[kAhead + 1];
@@ -332,10 +375,26 @@ struct Attention {
             for (int i = 0; i < 2 * NT; ++i) {
                 if (i + kAhead < 2 * NT) f[(i + kAhead) % (kAhead + 1)] = fragment(i + kAhead);
                 __builtin_amdgcn_sched_barrier(0);
-                const int qe = i % 2 == 0 ? q_exp : low_exp;
-                sc.s[0][i / 2] = mfma_codes(i / 2, a[0], f[i % (kAhead + 1)], sc.s[0][i / 2], e0, qe);
-                sc.s[1][i / 2] = mfma_codes(i / 2, a[1], f[i % (kAhead + 1)], sc.s[1][i / 2], e1, qe);
+                if (i % 2 == 0) {
+                    sc.s[0][i / 2] = mfma_codes<0>(i / 2, a[0], f[i % (kAhead + 1)], sc.s[0][i / 2], e0, q_exp);
+                    sc.s[1][i / 2] = mfma_codes<0>(i / 2, a[1], f[i % (kAhead + 1)], sc.s[1][i / 2], e1, q_exp);
+                } else {
+                    sc.s[0][i / 2] = mfma_codes<1>(i / 2, a[0], f[i % (kAhead + 1)], sc.s[0][i / 2], e0, low_exp);
+                    sc.s[1][i / 2] = mfma_codes<1>(i / 2, a[1], f[i % (kAhead + 1)], sc.s[1][i / 2], e1, low_exp);
+                }
                 __builtin_amdgcn_sched_barrier(0);
+            }
+            // (a loop over the marked tiles, not a test for each: 2 prompts of 8192 rows 1018 us against 1029, 32 of 512 773 against 787)
+            const int last_exp = q_exp - 0x01010101 * kLastExp;
+            for (int left = q_last; left; left &= left - 1) {
+                const int tile = __builtin_ctz(left) / 8;
+                const i32x8 part = parts(tile, 2);
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+                    if (n == tile) {
+                        sc.s[0][n] = mfma_codes<0>(n, a[0], part, sc.s[0][n], e0, last_exp);
+                        sc.s[1][n] = mfma_codes<0>(n, a[1], part, sc.s[1][n], e1, last_exp);
+                    }
             }
             return;
         }
@@ -683,19 +742,11 @@ struct Attention {
             h = u.head * p.group + tr.query(x);
         };
         bf16x8 q[kSharedQ ? 1 : NT][HD / 32];
-        State st;
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
+        const auto load_q = [&](int n, u32x4 (&w)[HD / 32]) {
             const int r = row_base + 16 * n + col;
             int token, h;
             row_of(16 * n + col, token, h);
-            st.m[n] = kNone;
-            st.l[n] = 0.f;
-#pragma unroll
-            for (int i = 0; i < D; ++i) st.o[n][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-            if (kSharedQ && n % kAttnWaves != wave) continue;
             const u16* src = p.q + (long long)(u.row0 + token) * p.ldq + h * HD + kg * 16;
-            u32x4 w[HD / 32];
 #pragma unroll
             for (int j = 0; j < HD / 32; ++j) {
                 w[j] = u32x4{0, 0, 0, 0};
@@ -703,26 +754,36 @@ struct Attention {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) w[j][i] = no_infinities(w[j][i] ^ p.q_sign);
             }
+        };
+        if constexpr (kSharedQ) {
+            static_assert(NT == kAttnWaves, "a wave prepares one row tile (by its number: unrolled, this would be a copy of cold code for every wave)");
+            u32x4 w[HD / 32];
+            load_q(wave, w);
             if constexpr (kCodesQ) {
-                u32x4 high[2], low[2];
-                unsigned int exponent;
-                split_q(w, high, low, exponent);
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    sh.q[n][i][lane] = high[i];
-                    sh.q[n][2 + i][lane] = low[i];
-                }
-                if (kg == 0) sh.q_exp[col][n] = (uint8_t)exponent;
+                split_q(w, sh, wave);
             } else {
 #pragma unroll
-                for (int j = 0; j < HD / 32; ++j) {
-                    if constexpr (kSharedQ) sh.q[n][j][lane] = w[j];
-                    else q[n][j] = __builtin_bit_cast(bf16x8, w[j]);
-                }
+                for (int j = 0; j < HD / 32; ++j) sh.q[wave][j][lane] = w[j];
+            }
+        } else {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                u32x4 w[HD / 32];
+                load_q(n, w);
+#pragma unroll
+                for (int j = 0; j < HD / 32; ++j) q[n][j] = __builtin_bit_cast(bf16x8, w[j]);
             }
         }
         if (kSharedQ) __syncthreads();
-        const int q_exp = kCodesQ ? *reinterpret_cast<const int*>(sh.q_exp[col]) : 0;
+        const int q_exp = kCodesQ ? *reinterpret_cast<const int*>(sh.q_exp[col]) : 0, q_last = kCodesQ ? uniform(*reinterpret_cast<const int*>(sh.q_last)) : 0;
+        State st;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            st.m[n] = kNone;
+            st.l[n] = 0.f;
+#pragma unroll
+            for (int i = 0; i < D; ++i) st.o[n][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
 
         constexpr int stride = ALONE ? kStep : kRound;
         int key = begin + (ALONE ? 0 : wave * kStep);
@@ -749,7 +810,7 @@ struct Attention {
                 if (more) w = find_step(hd, ids, next < end ? next : key, last_key, bad);
                 Scores sc;
                 __builtin_amdgcn_s_setprio(1);      // (the other waves of the SIMD have exponentials to do)
-                scores(s, q, q_exp, sh, sc);
+                scores(s, q, q_exp, q_last, sh, sc);
                 __builtin_amdgcn_s_setprio(0);
                 accumulate([&] { if (more) load_k(w, s); }, s.v, ok0, ok1, sc, e, tr, key, last_key, masked, p.c_log2, st);
                 if (more) load_v(p, w, s);
