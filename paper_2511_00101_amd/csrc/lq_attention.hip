@@ -1204,8 +1204,8 @@ extern "C" lq_status lora_cache_attention(const void* q, int64_t ldq, void* out,
     p.ldo = ldo;
     p.pages = static_cast<const uint8_t*>(pages);
     p.group = n_heads / kv;
-    // (not zero: a masked score is -infinity times this; 1e-30 of a score is as good as none of it)
-    p.c_log2 = __builtin_fmaxf(__builtin_fabsf(scale) * 1.44269504f, 1e-30f);
+    // (not zero: a masked score is -infinity times this; the least number above it times the largest score is below 2^-20)
+    p.c_log2 = __builtin_fmaxf(__builtin_fabsf(scale) * 1.44269504f, 1e-45f);
     p.group_magic = (unsigned)(((1 << 20) + p.group - 1) / p.group);
     p.q_sign = scale < 0.f ? 0x80008000u : 0u;
     const int nt = row_tiles(p.group, max_rows, n_seqs, kv);

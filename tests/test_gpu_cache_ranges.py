@@ -57,3 +57,37 @@ def test_two_elements_of_q_far_apart():
     for bound in (1, 30, 1000):
         out = base.attend(cache, q.cuda(), None, ints([0, n]), ints([0]), bound, scale=1.0)
         base.assert_attention(f64(out).reshape(n, 1, d), *want, n)
+
+
+@pytest.mark.parametrize("top", [1.0, 3.3e38, 1e-30, 2.0 ** -120])
+def test_rows_of_q_of_every_size(top):
+    """Rows whose elements reach from bf16's largest values down to its smallest normal ones, with a scale that brings the scores back."""
+    n, d, total = 20, 128, 100
+    rng = np.random.default_rng(3)
+    cache = base.make_cache(rng, [total], 1, d, 32)
+    huge = top > 1e30                                 # keys that keep the scores within fp32
+    k, v = bf16(rng, (total, d), 2.0 ** -20 if huge else 1.0), bf16(rng, (total, d))
+    base.store(cache, k.cuda(), v.cuda(), None, ints([0, total]), ints([0]))
+    K, V = base.load_all(cache, [total])
+    q = (torch.from_numpy(rng.uniform(-1, 1, (n, d))).double() * top).to(torch.bfloat16)
+    scale = 8 / top / d ** 0.5 * (2.0 ** 20 if huge else 1.0)
+    for bound in (1, 30, 1000):
+        out = base.attend(cache, q.cuda(), None, ints([0, n]), ints([total - n]), bound, scale=scale)
+        want = cm.attention(f64(q).reshape(n, 1, d), K[0], V[0], total - n, scale)
+        base.assert_attention(f64(out).reshape(n, 1, d), *want, total)
+
+
+@pytest.mark.parametrize("scale", [0.0, 1e-38, -3e-39, 2e-33])
+@pytest.mark.parametrize("bound", [1, 30, 1000])
+def test_tiny_scales_of_huge_scores(bound, scale):
+    """q . K of up to 2^120 and a scale that makes little or nothing of them."""
+    n, d, total = 20, 128, 100
+    rng = np.random.default_rng(4)
+    cache = base.make_cache(rng, [total], 1, d, 32)
+    k, v = bf16(rng, (total, d), 2.0 ** 100), bf16(rng, (total, d))
+    base.store(cache, k.cuda(), v.cuda(), None, ints([0, total]), ints([0]))
+    K, V = base.load_all(cache, [total])
+    q = bf16(rng, (n, d), 2.0 ** 15)
+    out = base.attend(cache, q.cuda(), None, ints([0, n]), ints([total - n]), bound, scale=scale)
+    want = cm.attention(f64(q).reshape(n, 1, d), K[0], V[0], total - n, float(np.float32(scale)))
+    base.assert_attention(f64(out).reshape(n, 1, d), *want, total)
