@@ -47,7 +47,7 @@ constexpr int kMaxRowWaves = 1 << 25;           // (a launch has fewer than 2^32
 // A span's blocks are found without a table of them: span s owns the items from row_starts[s] / 16 + 2 s on, which are enough
 // for n rows at any offset (at most (n + 14) / 16 + 1 blocks); the others have nothing to do.
 // Bound and measured (8 key heads of 128, in a graph): one row each of 256 sequences is a chain of five dependent round trips, 6.5 us to store and
-// 4.4 to read back for 15 MB; 12 prompts of up to 2048 rows by bandwidth, 12.1 and 11.8 us for 60 MB each (5.0 and 5.1 TB/s, the rate of
+// 4.7 to read back for 15 MB; 12 prompts of up to 2048 rows by bandwidth, 12.1 and 11.8 us for 60 MB each (5.0 and 5.1 TB/s, the rate of
 // a copy).  Storing, a block's elements are looked at as packed magnitudes and converted in pairs, the scale being an operand of the conversion;
 // with the elements widened to fp32 one by one the vector instructions took half of the cycles (8.0 and 15.0 us).
 // =================================================================================================
@@ -73,17 +73,25 @@ __device__ __forceinline__ bool find_block(const CacheView& c, const Spans& sp, 
     j.n = j.rows_ok ? end - j.row0 : 0;
     const int local = item - ((j.row0 >> 4) + 2 * s);
     const bool reach = bool(j.first >= 0) & bool(j.n <= c.max_len - j.first);
-    if (local < 0) return false;                       // (row_starts that decrease)
-    // (a span that cannot be used is reported by the wave of its first item)
-    if (local > 0 && (!j.rows_ok || !reach || local > ((j.first + j.n - 1) >> 4) - (j.first >> 4))) return false;
-    if (j.rows_ok && j.n == 0) return false;
-    j.rows_ok = j.rows_ok & reach;
+    if (local < 0 || j.n == 0) return false;           // (row_starts that decrease; no rows, or none inside the matrices)
+    // (a span whose positions cannot be used is reported by the wave of its first item)
+    if (local > 0 && (!reach || local > ((j.first + j.n - 1) >> 4) - (j.first >> 4))) return false;
+    j.rows_ok = reach;
     j.pos0 = j.rows_ok ? ((j.first >> 4) + local) * kBlock : 0;
     const int slot = min(max(j.slot, 0), c.n_slots - 1);
     j.len = c.lens[slot];
     j.page = c.table[(long long)slot * c.max_pages + (j.pos0 >> c.t_log2)];
     j.rows_ok = j.rows_ok & bool(j.slot == slot);
     return true;
+}
+// Spans whose rows are not inside the matrices, 64 by a wave behind those with items: no search needs to find one (row_starts that decrease, or
+// begin in front of the matrices), and the waves with items wait for nothing more (256 rows read back 4.3 -> 4.7 us, 8000 rows of one prompt 11.0 -> 10.5).
+__device__ __forceinline__ void report_rows(const CacheView& c, const Spans& sp, int wave)
+{
+    const int s = wave * kWave + lane_id();
+    if (s >= sp.n_seqs) return;
+    const int begin = sp.row_starts[s], end = sp.row_starts[s + 1];
+    if (begin < 0 || end < begin || end > sp.n_rows) atomicOr(c.err, kErrBadSegment);
 }
 __device__ __forceinline__ bool usable(const CacheView& c, BlockJob& j)
 {
@@ -214,7 +222,10 @@ __global__ __launch_bounds__(256) void store_rows_kernel(CacheView c, Spans sp, 
     constexpr int D = HD / 16, W = D / 4;       // elements per lane and position; words of codes of them
     const int wid = uniform((int)blockIdx.x * 4 + (int)threadIdx.x / kWave);
     const int item = wid / c.n_kv_heads, head = wid - item * c.n_kv_heads;
-    if (item >= n_items) return;
+    if (item >= n_items) {
+        report_rows(c, sp, wid - n_items * c.n_kv_heads);
+        return;
+    }
     BlockJob j;
     if (!find_block(c, sp, item, j)) return;
     const int lane = lane_id(), kg = lane >> 4, m = lane & 15;
@@ -367,7 +378,10 @@ __global__ __launch_bounds__(256) void load_rows_kernel(CacheView c, Spans sp, c
     constexpr int D = HD / 16, W = D / 4;
     const int wid = uniform((int)blockIdx.x * 4 + (int)threadIdx.x / kWave);
     const int item = wid / c.n_kv_heads, head = wid - item * c.n_kv_heads;
-    if (item >= n_items) return;
+    if (item >= n_items) {
+        report_rows(c, sp, wid - n_items * c.n_kv_heads);
+        return;
+    }
     BlockJob j;
     if (!find_block(c, sp, item, j)) return;
     const int lane = lane_id(), kg = lane >> 4, m = lane & 15;
@@ -964,7 +978,7 @@ lq_status move_cache_rows(void* k, int64_t ldk, void* v, int64_t ldv, int32_t n_
     if (!workspace || !aligned16(workspace) || workspace_bytes < LQ_CACHE_MIN_WORKSPACE) return LQ_ERR_WORKSPACE;
     if (n_seqs == 0 || n_rows == 0) return LQ_OK;
     const Spans sp{slots, row_starts, first, n_seqs, n_rows};
-    const dim3 grid((unsigned)((items * host_cache->n_kv_heads + 3) / 4)), block(256);
+    const dim3 grid((unsigned)((items * host_cache->n_kv_heads + (n_seqs + kWave - 1) / kWave + 3) / 4)), block(256);
     const hipStream_t hs = static_cast<hipStream_t>(stream);
     uint8_t* pg = static_cast<uint8_t*>(pages);
     if constexpr (STORE) {
