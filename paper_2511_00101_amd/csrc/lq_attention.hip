@@ -50,10 +50,12 @@ constexpr int kLeastChunk = 4 * kRound;
 template <int NT> constexpr int kSplitCost = NT == 1 ? 4 * kRound : 8 * kRound;
 constexpr int kAloneLongest = kLeastChunk;      // (not split, then)
 constexpr int kClasses = 5;
-// Spans that a workgroup keeps in LDS (16 bytes each; with four row tiles as many as leave room for two workgroups on a compute unit); of
-// more, a unit's is read again.
-template <int NT> constexpr int kKeptSpans = NT < 4 ? 1024 : 256;
 __host__ __device__ constexpr int span_at(int n) { return (3 * n + 1 + 3) / 4 * 4; }
+// Spans that a workgroup keeps in LDS (16 bytes each, beside the 12 that every span takes there); of more, a unit's is read again.  With one row tile some 690
+// spans (head_dim 64: 820) take the room of a workgroup, which costs less than reading them again would (1000 of up to 600 positions 98 us against
+// 100 and, with head_dim 64, 57 against 65); with four it would be one of two.
+template <int NT> constexpr int kKeptSpans = NT < 4 ? 1024 : 256;
+constexpr int kLdsBytes = 160 * 1024, kLdsGranule = 1280;       // of a compute unit; what a workgroup gets is a multiple
 constexpr float kNone = -3e38f;                 // a maximum before anything was seen: below every score, and finite (no case of its own anywhere)
 constexpr float kLazy = 8.f;                    // log2 of how far a score may exceed the maximum that its exponentials use
 constexpr int kAllButOrder = 0x4;              // what the scheduler may move across: scalar arithmetic
@@ -1127,26 +1129,39 @@ __global__ __launch_bounds__(kAttnThreads, (kResident<HD, NT>)) void attention_k
     }, 0, by_heads ? 8 : 1);
 }
 
-template <int NT>
-size_t prefix_bytes(int n_seqs) { return (size_t)span_at(n_seqs) * sizeof(int) + (n_seqs <= kKeptSpans<NT> ? (size_t)n_seqs * sizeof(Span) : 0); }
+template <int HD, int NT>
+constexpr int prefix_bytes(int n_seqs) { return span_at(n_seqs) * (int)sizeof(int) + (n_seqs <= kKeptSpans<NT> ? n_seqs * (int)sizeof(Span) : 0); }
+
+// Workgroups of a CU that the LDS has room for: the grid is no larger.  (A workgroup's first two units are its own, the longest first: one that only
+// starts when others are done ends last.  With kResident whatever the LDS holds: 1000 sequences of 600 positions 228 us, so 208; 2000 of up
+// to 60 87 and 72; but 700 of up to 4000, about as many units as the larger grid has places for, 369 and 410.)
+template <int HD, int NT>
+constexpr int resident(int n_seqs)
+{
+    const int bytes = (int)sizeof(typename Attention<HD, NT>::Shared) + prefix_bytes<HD, NT>(n_seqs);
+    const int room = kLdsBytes / ((bytes + kLdsGranule - 1) / kLdsGranule * kLdsGranule);
+    return room < kResident<HD, NT> ? room : kResident<HD, NT>;
+}
 
 template <int HD, int NT>
 hipError_t launch_attention(AttnParams p, int max_units, void* workspace, hipStream_t stream)
 {
+    static_assert(resident<HD, NT>(NT < 4 ? 512 : kKeptSpans<NT>) == kResident<HD, NT>, "no workgroup's room is taken by few spans");
+    static_assert(resident<HD, NT>(kKeptSpans<NT>) >= 1 && resident<HD, NT>(LQ_CACHE_MAX_SEQS) >= 1, "every call fits");
     static DeviceGrid cus;
     const int n_cu = cus.get([] {
         int dev = 0, n = 0;
         if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) n = 256;
         (void)hipFuncSetAttribute(reinterpret_cast<const void*>(attention_kernel<HD, NT>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                  (int)(prefix_bytes<NT>(LQ_CACHE_MAX_SEQS) > prefix_bytes<NT>(kKeptSpans<NT>) ? prefix_bytes<NT>(LQ_CACHE_MAX_SEQS) : prefix_bytes<NT>(kKeptSpans<NT>)));
+                                  max(prefix_bytes<HD, NT>(LQ_CACHE_MAX_SEQS), prefix_bytes<HD, NT>(kKeptSpans<NT>)));
         return n;
     });
-    const int grid = min(max_units, n_cu * kResident<HD, NT>);
+    const int grid = min(max_units, n_cu * resident<HD, NT>(p.sp.n_seqs)), lds = prefix_bytes<HD, NT>(p.sp.n_seqs);
     p.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + kWsHeaderBytes);
     p.partial_bytes = (unsigned)kSlots<NT> * slot_floats<HD, NT>() * 4;
     p.tickets = static_cast<int*>(workspace) + 4;
     p.arrivals = static_cast<uint8_t*>(workspace) + 4 * kArrivals;
-    hipLaunchKernelGGL((attention_kernel<HD, NT>), dim3(grid), dim3(kAttnThreads), prefix_bytes<NT>(p.sp.n_seqs), stream, p);
+    hipLaunchKernelGGL((attention_kernel<HD, NT>), dim3(grid), dim3(kAttnThreads), lds, stream, p);
     return hipGetLastError();
 }
 
