@@ -399,6 +399,8 @@ class PagedCache:
         assert all(t.dtype == torch.int32 and t.is_contiguous() for t in (table, lens, refs))
         assert table.dim() == 2 and lens.numel() == table.shape[0]
         n_bytes = lora_cache_page_bytes(n_kv_heads, head_dim, page_tokens)
+        if any(t.device != refs.device for t in (table, lens, *pages)):
+            raise ValueError("the table, the lengths or a layer's pages lie on another device than the reference counts")
         for p in pages:
             assert p.dtype == torch.uint8 and p.is_contiguous() and tuple(p.shape) == (refs.numel(), n_bytes)
         self.n_kv_heads, self.head_dim, self.page_tokens = n_kv_heads, head_dim, page_tokens
