@@ -401,7 +401,7 @@ lq_status lora_cache_compact(const lq_cache* host_cache, void* const* pools, int
                              size_t workspace_bytes, void* stream);
 
 /* Keys and values of a step's rows into the pages of one layer (`pages`).  k, v  bf16 [n_rows, n_kv_heads * head_dim], leading dimensions
- * ldk, ldv (multiples of 8, 16-byte aligned).  Per block and head, K and V each: e is the least integer with max |x| <= 448 * 2^e over
+ * ldk, ldv (multiples of 8, 16-byte aligned), two matrices (k == v is LQ_ERR_INVALID_ARG).  Per block and head, K and V each: e is the least integer with max |x| <= 448 * 2^e over
  * the block's new finite elements, within [-100, 119], and not below the block's exponent if the block holds positions before the
  * span's first (their codes are then brought to the new exponent); code = x * 2^-e rounded to nearest even e4m3, at most
  * +-448; NaN and infinities become NaN.  Sequences are stored in order: what a block held behind the span's last row is lost.

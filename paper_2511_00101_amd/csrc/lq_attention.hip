@@ -17,12 +17,13 @@
 // partial sums in chunk order.
 //
 // Bound and measured (8 key heads of 128 for 32 query heads unless stated):
-//   256 single tokens behind up to 4096 positions  131 us, 5.6 TB/s of codes: the rate of reading
+//   256 single tokens behind up to 4096 positions  132 us, 5.6 TB/s of codes; equally long ones of 2000 161 us, 6.6 TB/s: the rate of reading
 //   3 behind up to 32768, 32 key heads             47 us, 5.1 TB/s
 //   48 drafts of 5 rows behind up to 3000, d 64    21 us for 51 MB: 4 us until the first unit, 8 of a chunk's steps (a memory latency each), 4 of joins
-//   9 of up to 777 rows behind up to 2500          75 us, 0.61 PFLOP/s: three uneven units a workgroup, 6 us outside the steps each
-//   2 of 8192 rows                                 1.01 to 1.08 ms (by card), 1.02 to 1.09 PFLOP/s where a large product reaches 1.27: the vector
-//                                                  instructions of the softmax (64 % of the SIMDs' cycles) beside the matrix ones (49 %)
+//   9 of up to 777 rows behind up to 2500          75 us, 0.62 PFLOP/s: three uneven units a workgroup, 6 us outside the steps each
+//   2 of 8192 rows                                 1.02 to 1.05 ms (by card), 1.04 to 1.08 PFLOP/s where a large product reaches 1.24 to 1.27: the vector
+//                                                  instructions of the softmax (63 % of the SIMDs' cycles) beside the matrix ones (49 %); with
+//                                                  head_dim 64 0.72 ms, 0.76 PFLOP/s (69 % and 31 %)
 //   4 single tokens of up to 60 positions, d 64    7 us with its launch: round trips (spans, lengths, pages, codes)
 #include "lq_cache.h"
 #include "lq_internal.h"
@@ -40,7 +41,8 @@ constexpr int kArrivalBytes = kWsHeaderBytes - 4 * kArrivals;
 // Partial-sum slots of a call: a split tile has at least two, and its counter's number is its first slot's / 2.
 template <int NT> constexpr int kSlots = NT <= 2 ? 4 * kArrivalBytes : 2 * kArrivalBytes;
 constexpr int kManyChunksSlots = 2 * kArrivalBytes;    // with counters of eight bits
-// workgroups of a CU: as many as the accumulators, the codes of a step and Q leave registers for without spilling
+// Workgroups of a CU: as many as the accumulators, the codes of a step and Q leave registers for in the loop over the steps, where nothing spills.
+// (Outside it four tiles of head_dim 128 keep 11 vector registers in memory, and every kernel 51 to 69 scalar ones in lanes of vector registers.)
 template <int HD, int NT> constexpr int kResident = HD == 64 ? (NT == 1 ? 4 : NT == 2 ? 3 : 2) : NT == 1 ? 3 : 2;
 // (us, half as long and twice as long beside it: 8 drafts of 8 rows behind up to 6000 positions 24.2, 21.0, 22.0; one token behind 3000 11.6, 12.8,
 // 14.5, behind 30000 25.7, 23.2, 21.8)
@@ -176,7 +178,7 @@ struct Attention {
     // of rows of codes: q = 2^e (high + low 2^-11 + last 2^-22), one e a row, high and last in e4m3, low in e5m2.  Of a bf16 value's
     // eight bits high takes four and low the other three (a nearest one's remainder has a sign); where the row's largest element is more than 2^14
     // times larger, high loses bits, and last has what low cannot hold: the sum is exact down to 2^-31 of the largest element, and off by at most
-    // 2^-39 of it below (and of 2^-97 in rows that are smaller).  Last is multiplied only for row tiles that have one (of Gaussian rows one of eleven; 1.5 % of the
+    // 2^-39 of it below (and of 2^-97 in rows that are smaller).  Last is multiplied only for row tiles that have one (of Gaussian rows one of eleven; 1.7 % of the
     // time of two 8192-row prompts).  Two 16 x 16 x 128 products take what four bf16 ones take, without the conversion of K (two prompts of 8192 rows 1137 us
     // against 1241 when it was brought in).  With head_dim 64 one product of the depth 128 would hold both parts, but K's duplicated halves have to be
     // exchanged between lanes, as many instructions as the conversion.
@@ -386,7 +388,7 @@ struct Attention {
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
-            // (a loop over the marked tiles, not a test for each: 2 prompts of 8192 rows 1018 us against 1029, 32 of 512 773 against 787)
+            // (a loop over the marked tiles, not a test for each: 2 prompts of 8192 rows 1018 us against 1023, 32 of 512 behind 2560 773 against 789)
             const int last_exp = q_exp - 0x01010101 * kLastExp;
             for (int left = q_last; left; left &= left - 1) {
                 const int tile = __builtin_ctz(left) / 8;
@@ -1168,8 +1170,8 @@ hipError_t launch_attention(AttnParams p, int max_units, void* workspace, hipStr
 // Row tiles of 16 of a unit: a group of query heads of one token, a draft, or a prompt.  Four tiles widen every code for 64 rows and
 // cost 3 us more to set up and to join: where units of two tiles do not fill the compute units, those are faster by that behind few
 // positions, and lose it only behind thousands (us, two tiles against four: 16 spans of 16 rows of 4 heads behind 300 positions 12.0 and
-// 15.3, behind 2000 28.2 and 29.1; one of 64 rows behind 1000 16.3 and 20.4, behind 12000 36.5 and 38.5, behind 30000 64 and 55; but 20 spans of
-// 16 rows, 320 units, behind 2000 33.5 and 30.3; 60 of 14 x 3 rows for 16 key heads, 1920 units, 37 and 26).
+// 15.4, behind 2000 28.6 and 29.5; one of 64 rows behind 1000 16.6 and 22.0, behind 12000 37.4 and 37.5, behind 30000 62 and 54; but 20 spans of
+// 16 rows, 320 units, behind 2000 34.1 and 30.5; 60 of 14 x 3 rows for 16 key heads, 1920 units, 38 and 27).
 int row_tiles(int group, int max_rows, int n_seqs, int kv_heads)
 {
     const long long rows = (long long)group * max_rows;

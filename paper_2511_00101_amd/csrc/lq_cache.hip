@@ -46,10 +46,11 @@ constexpr int kMaxRowWaves = 1 << 25;           // (a launch has fewer than 2^32
 // of the four groups is four whole rows, and a lane has the four positions that a word of V's layout takes together.
 // A span's blocks are found without a table of them: span s owns the items from row_starts[s] / 16 + 2 s on, which are enough
 // for n rows at any offset (at most (n + 14) / 16 + 1 blocks); the others have nothing to do.
-// Bound and measured (8 key heads of 128, in a graph): one row each of 256 sequences is a chain of five dependent round trips, 6.5 us to store and
-// 4.7 to read back for 15 MB; 12 prompts of up to 2048 rows by bandwidth, 12.1 and 11.8 us for 60 MB each (5.0 and 5.1 TB/s, the rate of
-// a copy).  Storing, a block's elements are looked at as packed magnitudes and converted in pairs, the scale being an operand of the conversion;
-// with the elements widened to fp32 one by one the vector instructions took half of the cycles (8.0 and 15.0 us).
+// Bound and measured (8 key heads of 128; a store and a load in turn, and in brackets either repeated alone in a graph): one row each of 256 sequences is a chain
+// of five dependent round trips, 7.0 us to store (6.6) and 6.6 to read back (4.7) for 15 MB; 12 prompts of up to 2048 rows by bandwidth, 15.3 (12.0) and 12.2 us
+// (11.7) for 60 MB each: 3.9 and 4.9 TB/s where a copy reaches 5.1.  Storing, a block's elements are looked at as packed magnitudes and converted in pairs,
+// the scale being an operand of the conversion; with the elements widened to fp32 one by one the vector instructions took half of the cycles (alone 8.0 and
+// 15.0 us to store).
 // =================================================================================================
 // A wave's start is a chain of dependent round trips (spans, span, table and rows, page); nothing of a trip waits for a check of the one
 // before: indexes are brought into range instead, and what was found is looked at when all of it is there.
