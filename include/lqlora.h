@@ -425,7 +425,7 @@ lq_status lora_cache_load_rows(void* k, int64_t ldk, void* v, int64_t ldv, int32
  *            it: long tiles hold q as a sum of 8-bit parts.
  *            An element of q that is not finite makes its row and head NaN (where it sees a position).  Scores lie within fp32's range.
  *   max_rows the largest number of rows of a span (a bound from above will do): picks the kernel's tile, no result depends on
- *            it but for the order of sums
+ *            it but for the order of sums (and for q's elements below 2^-31, see q)
  *   A position that a row does not see leaves no trace in it (NaN included); a row that sees no usable page is zero.
  *   n_seqs up to LQ_CACHE_MAX_SEQS, n_rows up to LQ_CACHE_MAX_ROWS.  Results are the same from run to run. */
 #define LQ_CACHE_MAX_SEQS 4096
